@@ -169,6 +169,77 @@ int sigmoid_attn_bwd_dq_dbias_static(const void *q, const void *k, const void *v
                                      float *dbias, const int32_t *seqlens, const float *bias, float scale,
                                      int B, int N_max, int H, int d, void *stream);
 
+/*
+ * A learned relative position bias, by buckets, and its gradient.  Lengths and layouts as for sigmoid_attn_cross_fwd / _bwd.
+ *
+ *     x_ij = scale <q_i, k_j> + bias[z] + table[b_ij][h],   b_ij = buckets[clamp(j - i - q_start[z], -reach, reach) + reach]
+ *     dtable[b][h] = sum over z and valid i, j with b_ij = b of dS_ij      (0 for a bucket that no valid pair has)
+ *
+ *   table, dtable : in / out, device bf16 [num_buckets, H], at least 2-byte aligned; dtable is fully overwritten
+ *   buckets       : device int32 [2 * reach + 1]; values outside [0, num_buckets) are clamped inside the kernels
+ *   q_start       : device int32 [B], the position of query row 0 of each sequence among its keys, or NULL for zeros (self-attention);
+ *                   with it a call takes the last tokens of a context alone.  Clamped to +-2^29.
+ * reach is 0 to 2^24, num_buckets 1 to 65536, L_q and L_k at most 2^29.  An entry of -inf (or the type's lowest value) masks its pairs: P and dS are exact zeros.
+ * Entries that no valid pair has influence no output, NaN ones neither.
+ * The workspace of the backward call (sigmoid_attn_rel_bwd_workspace_bytes(...) bytes, 16-byte aligned, owned by the caller, contents
+ * irrelevant on entry and undefined on exit) holds a row of sums by distance for every 32 queries; sums are taken in fp32, in an
+ * order that the shapes and the valid lengths fix: results are bitwise reproducible.  Calls whose kernels may overlap need workspaces of their own.
+ */
+int sigmoid_attn_rel_fwd(const void *q, const void *k, const void *v, void *o,
+                         const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+                         const void *table, const int32_t *buckets, int num_buckets, int reach, const int32_t *q_start,
+                         int B, int L_q, int L_k, int H, int d, void *stream);
+size_t sigmoid_attn_rel_bwd_workspace_bytes(int B, int L_q, int L_k, int H, int d, int reach);
+int sigmoid_attn_rel_bwd(const void *q, const void *k, const void *v, const void *d_o,
+                         void *dq, void *dk, void *dv, void *dtable,
+                         const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+                         const void *table, const int32_t *buckets, int num_buckets, int reach, const int32_t *q_start,
+                         int B, int L_q, int L_k, int H, int d, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A map of distances to buckets, written to HOST memory int32 [2 * reach + 1] (entry t + reach is that of distance t): a bucket for
+ * every distance if there are enough; else half of the buckets for each sign (the larger half of the numbers for keys behind the
+ * query), of these half for single distances from 0 on and the others spaced by the logarithm up to reach.
+ * Any other map will do as well.
+ */
+int sigmoid_attn_rel_buckets(int32_t *buckets, int num_buckets, int reach);
+
+/*
+ * Dropout of the attention weights, its mask made anew in every pass and never stored.  Lengths and layouts as for sigmoid_attn_cross_fwd / _bwd.
+ *
+ *     O_i = sum_j m_ij P_ij v_j / keep,   dV_j = sum_i m_ij P_ij dO_i / keep,   dS_ij = P_ij (1 - P_ij) m_ij dP_ij / keep
+ *
+ *   p   : 0 <= p < 1; K = floor((1 - p) 65536 + 1/2) (at least 1) of 65536 weights stay, keep = K / 65536.  K = 65536 drops nothing, and the
+ *         call is the one without dropout.
+ *   rng : device uint64 [2], 8-byte aligned: seed and offset.  The backward call takes what the forward call took; a program
+ *         changes the offset from step to step (in device memory, so that a captured graph can too).
+ *
+ * m_ij depends on seed, offset (modulo 2^32), z H + h, i and j alone, and is defined bit by bit: Philox4x32 with seven rounds (Salmon, Moraes, Dror,
+ * Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011), key (seed mod 2^32, seed div 2^32), counter
+ * (i, 2 (j div 32) + (j div 4) mod 2, z H + h, offset mod 2^32), gives words r0..r3.  With e = j mod 2 and w = 2 ((j mod 32) div 8) + (j div 2) mod 2 the
+ * weight takes bits t = w + 16 e and t + 8 of each word, as the byte a(t) = sum_s 2^s bit(t + 8 (s mod 2), r_(s div 2)), s = 0..7, and
+ * m_ij = 1 where 256 a(t) + reversed(a(t xor 16)) + K >= 65536, reversed() turning the order of the eight bits around.
+ */
+int sigmoid_attn_dropout_fwd(const void *q, const void *k, const void *v, void *o,
+                             const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+                             float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream);
+int sigmoid_attn_dropout_bwd(const void *q, const void *k, const void *v, const void *d_o,
+                             void *dq, void *dk, void *dv,
+                             const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+                             float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream);
+
+/* Both at once; the workspace is that of sigmoid_attn_rel_bwd. */
+int sigmoid_attn_rel_dropout_fwd(const void *q, const void *k, const void *v, void *o,
+                                 const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+                                 const void *table, const int32_t *buckets, int num_buckets, int reach, const int32_t *q_start,
+                                 float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream);
+int sigmoid_attn_rel_dropout_bwd(const void *q, const void *k, const void *v, const void *d_o,
+                                 void *dq, void *dk, void *dv, void *dtable,
+                                 const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+                                 const void *table, const int32_t *buckets, int num_buckets, int reach, const int32_t *q_start,
+                                 float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
 /* Scratch bytes sigmoid_attn_bwd needs for this shape (0 on invalid shapes). */
 size_t sigmoid_attn_bwd_workspace_bytes(int B, int N_max, int H, int d);
 

@@ -27,7 +27,9 @@ EXPORTS = ("sigmoid_attn_version", "sigmoid_attn_strerror", "sigmoid_attn_fwd", 
            "sigmoid_attn_cross_fwd", "sigmoid_attn_cross_bwd",
            "sigmoid_attn_bwd_dq_dbias", "sigmoid_attn_bwd_dq_dbias_workspace_bytes",
            "sigmoid_attn_cross_bwd_dq_dbias", "sigmoid_attn_cross_bwd_dq_dbias_workspace_bytes",
-           "sigmoid_attn_bwd_dq_dbias_static")
+           "sigmoid_attn_bwd_dq_dbias_static",
+           "sigmoid_attn_rel_fwd", "sigmoid_attn_rel_bwd", "sigmoid_attn_rel_bwd_workspace_bytes", "sigmoid_attn_rel_buckets",
+           "sigmoid_attn_dropout_fwd", "sigmoid_attn_dropout_bwd", "sigmoid_attn_rel_dropout_fwd", "sigmoid_attn_rel_dropout_bwd")
 
 _lib = None
 _fast = None            # the module _fastcall, or _NoFastCalls where it is not built; bound to the loaded library
@@ -113,6 +115,16 @@ def load() -> ctypes.CDLL:
         lib.sigmoid_attn_bwd_workspace_bytes.restype = sz
         lib.sigmoid_attn_bwd_onepass_workspace_bytes.argtypes = [ci, ci, ci, ci]
         lib.sigmoid_attn_bwd_onepass_workspace_bytes.restype = sz
+        rel, drop, sizes = [vp, vp, ci, ci, vp], [cf, vp], [ci] * 5
+        lib.sigmoid_attn_rel_buckets.argtypes = [vp, ci, ci]
+        lib.sigmoid_attn_rel_bwd_workspace_bytes.argtypes = sizes + [ci]
+        lib.sigmoid_attn_rel_bwd_workspace_bytes.restype = sz
+        lib.sigmoid_attn_rel_fwd.argtypes = [vp] * 7 + [cf] + rel + sizes + [vp]
+        lib.sigmoid_attn_rel_bwd.argtypes = [vp] * 11 + [cf] + rel + sizes + [vp, sz, vp]
+        lib.sigmoid_attn_dropout_fwd.argtypes = [vp] * 7 + [cf] + drop + sizes + [vp]
+        lib.sigmoid_attn_dropout_bwd.argtypes = [vp] * 10 + [cf] + drop + sizes + [vp]
+        lib.sigmoid_attn_rel_dropout_fwd.argtypes = [vp] * 7 + [cf] + rel + drop + sizes + [vp]
+        lib.sigmoid_attn_rel_dropout_bwd.argtypes = [vp] * 11 + [cf] + rel + drop + sizes + [vp, sz, vp]
         _lib = lib
     return _lib
 
@@ -403,3 +415,133 @@ def sigmoid_attn_cross_bwd_dq_dbias(q, k, v, d_o, seqlens_q, seqlens_k, bias, sc
     if rc != SIGATTN_OK:
         raise SigAttnError(rc)
     return dq, dbias
+
+
+# ---- a relative position bias, dropout of the attention weights, and both.  One function marshals the calls of each direction.
+def sigmoid_attn_rel_buckets(num_buckets: int, reach: int):
+    """A map of distances to buckets (int32 [2 * reach + 1], on the CPU): near distances by themselves, far ones by their logarithm."""
+    if not 0 <= reach <= 1 << 24:
+        raise ValueError("reach must be 0 to 2^24")
+    out = torch.empty(2 * reach + 1, dtype=torch.int32)
+    rc = load().sigmoid_attn_rel_buckets(out.data_ptr(), num_buckets, reach)
+    if rc != SIGATTN_OK:
+        raise SigAttnError(rc)
+    return out
+
+
+def sigmoid_attn_rel_bwd_workspace_bytes(B: int, L_q: int, L_k: int, H: int, d: int, reach: int) -> int:
+    return int(load().sigmoid_attn_rel_bwd_workspace_bytes(B, L_q, L_k, H, d, reach))
+
+
+def _same_device(like, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, q on {like.device}")
+
+
+def _check_rel(q, table, buckets, q_start):
+    """The arguments (table, buckets, num_buckets, reach, q_start) of a call."""
+    B, H = q.shape[0], q.shape[2]
+    if not (table.is_cuda and table.dtype == torch.bfloat16 and table.is_contiguous() and table.dim() == 2 and table.shape[1] == H):
+        raise ValueError("table must be a contiguous CUDA bf16 tensor of shape [num_buckets, H]")
+    if not (buckets.is_cuda and buckets.dtype == torch.int32 and buckets.is_contiguous() and buckets.dim() == 1 and buckets.shape[0] % 2 == 1):
+        raise ValueError("buckets must be a contiguous CUDA int32 tensor of shape [2 * reach + 1]")
+    if q_start is not None:
+        _check_vec(q_start, "q_start", B, torch.int32)
+    _same_device(q, table=table, buckets=buckets, q_start=q_start)
+    return (table.data_ptr(), buckets.data_ptr(), table.shape[0], (buckets.shape[0] - 1) // 2,
+            0 if q_start is None else q_start.data_ptr())
+
+
+def _check_drop(q, p, rng):
+    if not (rng.is_cuda and rng.dtype == torch.int64 and rng.is_contiguous() and rng.shape == (2,)):
+        raise ValueError("rng must be a contiguous CUDA int64 tensor (seed, offset)")
+    _same_device(q, rng=rng)
+    return float(p), rng.data_ptr()
+
+
+def _mod_fwd(name, q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, out, stream):
+    _check_cross(q, k, v)
+    B, Lq, H, d = q.shape
+    Lk = k.shape[1]
+    _check_vec(seqlens_q, "seqlens_q", B, torch.int32)
+    _check_vec(seqlens_k, "seqlens_k", B, torch.int32)
+    _check_vec(bias, "bias", B, torch.float32)
+    _same_device(q, k=k, v=v, seqlens_q=seqlens_q, seqlens_k=seqlens_k, bias=bias, out=out)
+    more = (_check_rel(q, *rel) if rel else ()) + (_check_drop(q, *drop) if drop else ())
+    with torch.cuda.device(q.device):
+        out = _output(out, "out", q)
+        rc = getattr(load(), name)(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), seqlens_q.data_ptr(), seqlens_k.data_ptr(),
+                                   bias.data_ptr(), float(scale), *more, B, Lq, Lk, H, d, _stream_ptr(stream))
+    if rc != SIGATTN_OK:
+        raise SigAttnError(rc)
+    return out
+
+
+def _mod_bwd(name, q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, rel, drop, dq, dk, dv, dtable, workspace, stream):
+    _check_cross(q, k, v)
+    _check(d_o, "d_o", q.shape)
+    B, Lq, H, d = q.shape
+    Lk = k.shape[1]
+    _check_vec(seqlens_q, "seqlens_q", B, torch.int32)
+    _check_vec(seqlens_k, "seqlens_k", B, torch.int32)
+    _check_vec(bias, "bias", B, torch.float32)
+    _same_device(q, k=k, v=v, d_o=d_o, seqlens_q=seqlens_q, seqlens_k=seqlens_k, bias=bias, dq=dq, dk=dk, dv=dv, dtable=dtable)
+    more = (_check_rel(q, *rel) if rel else ()) + (_check_drop(q, *drop) if drop else ())
+    with torch.cuda.device(q.device):
+        dq, dk, dv = _output(dq, "dq", q), _output(dk, "dk", k), _output(dv, "dv", k)
+        grads, scratch = (dq, dk, dv), ()
+        if rel:
+            if dtable is None:
+                dtable = torch.empty_like(rel[0])
+            elif not (dtable.dtype == torch.bfloat16 and dtable.is_contiguous() and dtable.shape == rel[0].shape):
+                raise ValueError("dtable must be a contiguous CUDA bf16 tensor of the table's shape")
+            grads += (dtable,)
+            need = sigmoid_attn_rel_bwd_workspace_bytes(B, Lq, Lk, H, d, more[3])
+            if workspace is None:
+                workspace = _scratch(max(need, 16), q, stream)
+                if workspace is None:
+                    raise RuntimeError(f"no {need} bytes for the workspace of this call and stream: pass one")
+            scratch = _workspace_args(workspace, q)
+        rc = getattr(load(), name)(q.data_ptr(), k.data_ptr(), v.data_ptr(), d_o.data_ptr(), *(t.data_ptr() for t in grads),
+                                   seqlens_q.data_ptr(), seqlens_k.data_ptr(), bias.data_ptr(), float(scale), *more, B, Lq, Lk, H, d,
+                                   *scratch, _stream_ptr(stream))
+    if rc != SIGATTN_OK:
+        raise SigAttnError(rc)
+    return grads
+
+
+def sigmoid_attn_rel_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, out=None, stream=None):
+    """Forward pass with table[buckets[clamp(j - i - q_start, -reach, reach) + reach]][h] added to the scores.
+    table: bf16 [num_buckets, H]; buckets: int32 [2 * reach + 1] (sigmoid_attn_rel_buckets makes one); q_start: int32 [B] or None."""
+    return _mod_fwd("sigmoid_attn_rel_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), None, out, stream)
+
+
+def sigmoid_attn_rel_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, dq=None, dk=None, dv=None,
+                         dtable=None, workspace=None, stream=None) -> Tuple:
+    """(dQ, dK, dV, dtable) of sigmoid_attn_rel_fwd.  Outputs and the workspace are allocated if None."""
+    return _mod_bwd("sigmoid_attn_rel_bwd", q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), None, dq, dk, dv, dtable,
+                    workspace, stream)
+
+
+def sigmoid_attn_dropout_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, p: float, rng, out=None, stream=None):
+    """Forward pass with dropout of the attention weights.  rng: int64 [2] in device memory, seed and offset."""
+    return _mod_fwd("sigmoid_attn_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, None, (p, rng), out, stream)
+
+
+def sigmoid_attn_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, p: float, rng, dq=None, dk=None, dv=None, stream=None) -> Tuple:
+    """(dQ, dK, dV) of sigmoid_attn_dropout_fwd with the same p, seed and offset."""
+    return _mod_bwd("sigmoid_attn_dropout_bwd", q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, None, (p, rng), dq, dk, dv, None, None, stream)
+
+
+def sigmoid_attn_rel_dropout_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, table, buckets, p: float, rng, q_start=None, out=None,
+                                 stream=None):
+    """Forward pass with the relative position bias and dropout."""
+    return _mod_fwd("sigmoid_attn_rel_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), (p, rng), out, stream)
+
+
+def sigmoid_attn_rel_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, p: float, rng, q_start=None, dq=None,
+                                 dk=None, dv=None, dtable=None, workspace=None, stream=None) -> Tuple:
+    """(dQ, dK, dV, dtable) of sigmoid_attn_rel_dropout_fwd."""
+    return _mod_bwd("sigmoid_attn_rel_dropout_bwd", q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), (p, rng), dq, dk, dv,
+                    dtable, workspace, stream)

@@ -5,12 +5,14 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsigattn.so")
-SOURCES = ["sigattn_api.hip"]
+SOURCES = ["sigattn_api.hip", "sigattn_mod_api.hip", "sigattn_rel.hip", "sigattn_dropout.hip", "sigattn_rel_dropout.hip"]
 PROBE_LIB = os.path.join(HERE, "libmachine_probes.so")  # measurement aids for the benchmark, a library of their own
 PROBE_SOURCES = ["machine_probes.hip"]
 
@@ -30,16 +32,28 @@ def hipcc() -> str:
     return exe
 
 
-def _compile(lib: str, sources, verbose: bool) -> str:
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", lib,
-           *[os.path.join(CSRC, s) for s in sources]]
+def _run(cmd, what: str, verbose: bool) -> None:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode != 0:
         print(" ".join(cmd))
         print(res.stdout)
         print(res.stderr)
     if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed building {os.path.basename(lib)}")
+        raise RuntimeError(f"hipcc failed building {what}")
+
+
+def _compile(lib: str, sources, verbose: bool) -> str:
+    """One object for each source, side by side, and the library from them."""
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in sources]
+
+        def one(pair):
+            _run([hipcc(), *flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", "-o", pair[1], os.path.join(CSRC, pair[0])], pair[0], verbose)
+
+        with ThreadPoolExecutor(max_workers=min(len(sources), int(os.environ.get("MAX_JOBS", 8)))) as pool:
+            list(pool.map(one, zip(sources, objects)))
+        _run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", lib, *objects], os.path.basename(lib), verbose)
     return lib
 
 

@@ -172,6 +172,17 @@ struct TrLayout {
     }
 };
 
+// Order in which a step uses its A operands: position -> operand, the score operands [0, NA) first.
+template <class C, bool BIASED>
+struct OperandOrder {
+    static constexpr int EARLY = BIASED && !C::HAS2 ? C::NC / 2 : 0;               // output operands in front of the scores
+    static constexpr int op(int pos) { return pos < EARLY ? C::NA + pos : pos < EARLY + C::NA ? pos - EARLY : pos; }
+    static constexpr bool score(int pos) { return op(pos) < C::NA; }
+    // of score operand j: its part of the head dimension, its score tile (0: S, 1: dP)
+    static constexpr int ks(int j) { return BIASED && C::HAS2 ? j % C::KS : j / C::NT; }
+    static constexpr int which(int j) { return BIASED && C::HAS2 ? 1 - j / C::KS : j % C::NT; }
+};
+
 // The VALU instructions of one step as a flat list.  Each unit (two score elements) runs through three
 // stages -- exponentials | denominator and reciprocal | products and packing -- and the list is skewed by
 // one unit per stage, so that an instruction never follows directly on the one that feeds it.
@@ -466,15 +477,25 @@ __device__ __forceinline__ bf16_t *uniform_ptr(const bf16_t *p) {
     return reinterpret_cast<bf16_t *>((unsigned long long)hi << 32 | lo);
 }
 
+// What run_pass() takes in where scores and weights are changed on their way (sigattn_mod.hpp has such types); this one changes nothing.
+struct Plain {
+    static constexpr bool BIASED = false;          // score accumulators start from values of the type's own, not from zeros
+    static constexpr bool SIFTED = false;          // weights of a finished block pass through the type before they are contracted
+    static constexpr bool SUMMED = false;          // dS of a finished block is looked at (DQ)
+    __device__ __forceinline__ float scale() const { return 1.0f; }
+};
+
 // The owner tiles of one workgroup, one pass.  `smem`: Cfg::LDS_BYTES bytes.
-template <int MODE, int D, int QB, int NW, int BN, int LD1, int LD2, int RING, bool WITH_DB>
-__device__ __forceinline__ void run_pass(const Params &p, const Work work, unsigned char *const smem, float *const s_db) {
+template <int MODE, int D, int QB, int NW, int BN, int LD1, int LD2, int RING, bool WITH_DB, class Mod = Plain>
+__device__ __forceinline__ void run_pass(const Params &p, const Work work, unsigned char *const smem, float *const s_db, Mod mod = Mod{}) {
     static_assert(!WITH_DB || MODE == DQ, "the bias gradient rides on the dQ kernel");
+    static_assert(!WITH_DB || !Mod::SUMMED, "one sum of dS at a time");
     using C = Cfg<MODE, D, QB, NW, BN, LD1, LD2, RING>;
     constexpr bool HAS2 = C::HAS2;
     constexpr int Q2 = HAS2 ? QB : 1;
     constexpr int NB = C::NB, NA = C::NA, NOPS = C::NOPS, SLOTS = C::SLOTS, NT = C::NT, NO = C::NO, MB = C::MB;
     constexpr float LOG2E = 1.4426950408889634f;
+    using Order = OperandOrder<C, Mod::BIASED>;
 
     bf16_t *y1s = reinterpret_cast<bf16_t *>(smem);                 // [NBUF][BN][LD1]
     bf16_t *y2s = y1s + C::NBUF * BN * LD1;                         // [NBUF][BN][LD2]
@@ -638,6 +659,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             st1[it] = __builtin_amdgcn_raw_buffer_load_b128(d1, (int)ld_off0, it * (int)pass_bytes, 0);
             st2[it] = __builtin_amdgcn_raw_buffer_load_b128(d2, (int)ld_off0, it * (int)pass_bytes, 0);
         }
+        if constexpr (Mod::BIASED) mod.request();
         next1 += (size_t)BN * row_stride;
         next2 += (size_t)BN * row_stride;
         rows_left = rows_left > BN ? rows_left - BN : 0;
@@ -676,6 +698,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             *reinterpret_cast<u32x4 *>(w1 + (slot * BN + it * RPI) * LD1) = st1[it];
             *reinterpret_cast<u32x4 *>(w2 + (slot * BN + it * RPI) * LD2) = st2[it];
         }
+        if constexpr (Mod::BIASED) mod.store();
     };
 
     // lane-constant pieces of the LDS addresses
@@ -698,15 +721,18 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     // The J-th A operand counted from the start of the step on block nb of `slot` (J >= NOPS runs into the
     // following step): row-wise operands belong to the block after the step's block, transposed ones to the
     // block before it.
+    // Operands are numbered in the order of use: score contractions (two score tiles in turn), then output contractions.
+    // BIASED: what a score tile starts from is read at the start of the step, and other contractions are in front of those that
+    // need it: the dP tile's, or in the forward pass half of the output's.
     auto fetch = [&](auto J_, auto slot, auto nb_c) -> bf16x8 {
         constexpr int J = decltype(J_)::value;
-        constexpr int sstep = J / NOPS, j = J % NOPS;
+        constexpr int sstep = J / NOPS, j = Order::op(J % NOPS);
         constexpr int blk = decltype(nb_c)::value + sstep + (j < NA ? 1 : -1) + NB;   // >= 0, counted from the previous tile
         constexpr int tile = blk / NB - 1;                                            // relative to the current one
         constexpr int brow = (blk % NB) * 32;
         const int row = ((slot.get() + tile) & (C::NBUF - 1)) * BN + brow;
         if constexpr (j < NA) {
-            constexpr int ks = j / NT, which = j % NT;
+            constexpr int ks = Order::ks(j), which = Order::which(j);
             if constexpr (which == 0) return lds_read_rows(rd1 + row * LD1 + 16 * ks);
             else return lds_read_rows(rd2 + row * LD2 + 16 * ks);
         } else {
@@ -754,7 +780,16 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
 
         static_for<0, SLOTS>([&](auto k_) {
             constexpr int k = decltype(k_)::value;
-            constexpr int j = k / QB, qb = k % QB;
+            constexpr int pos = k / QB, qb = k % QB, j = Order::op(pos);
+            if constexpr (Mod::SIFTED) {
+                if constexpr (!DRAIN) mod.template slot<k, SLOTS>();
+            }
+            if constexpr (Mod::BIASED) {
+                if constexpr (HAS_NEXT && !DRAIN && k == 0) {
+                    static_for<0, QB>([&](auto q_) { mod.template start<decltype(q_)::value>(sbuf[PAR ^ 1][decltype(q_)::value]); });
+                    mod.advance();
+                }
+            }
             // The two waves of a SIMD compete for its issue port, and the older one always wins: it reached the tile
             // barrier early and left the other to finish alone, at the poor rate of a lone wave.  Priorities that
             // fall with every quarter of a tile let the wave that is behind catch up: as fast as no barrier at all
@@ -771,18 +806,18 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             // ---- the MFMA of this slot
             if constexpr (j < NA) {
                 if constexpr (HAS_NEXT && !DRAIN) {
-                    constexpr int ks = j / NT, which = j % NT;
+                    constexpr int ks = Order::ks(j), which = Order::which(j);
                     if constexpr (which == 0)
                         sbuf[PAR ^ 1][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            ring[(G0 + j) % RING], xa[qb][ks], ks == 0 ? zero : sbuf[PAR ^ 1][qb], 0, 0, 0);
+                            ring[(G0 + pos) % RING], xa[qb][ks], ks == 0 && !Mod::BIASED ? zero : sbuf[PAR ^ 1][qb], 0, 0, 0);
                     else
                         dbuf[PAR ^ 1][HAS2 ? qb : 0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            ring[(G0 + j) % RING], xb[HAS2 ? qb : 0][HAS2 ? ks : 0],
+                            ring[(G0 + pos) % RING], xb[HAS2 ? qb : 0][HAS2 ? ks : 0],
                             ks == 0 ? zero : dbuf[PAR ^ 1][HAS2 ? qb : 0], 0, 0, 0);
                 }
             } else if constexpr (HAS_PREV) {
                 constexpr int jj = j - NA, which = jj % NO, idx = jj / NO, half = idx / MB, mb = idx % MB;
-                const bf16x8 a = ring[(G0 + j) % RING];
+                const bf16x8 a = ring[(G0 + pos) % RING];
                 if constexpr (MODE == FWD) {            // O^T += V^T P^T
                     acc0[qb][mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                         a, __builtin_bit_cast(bf16x8, pbuf[PAR ^ 1][qb][half]), acc0[qb][mb], 0, 0, 0);
@@ -799,10 +834,11 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 }
             }
             // ---- the register of the previous operand is free now: request the operand RING - 1 ahead
-            constexpr int ahead = j + RING - 1;         // those of contractions that are not made are not read
-            constexpr bool wanted = ahead < NA ? HAS_NEXT : (ahead < NOPS ? HAS_PREV : !DRAIN && (HAS_NEXT || ahead >= NOPS + NA));
+            constexpr int ahead = pos + RING - 1;       // those of contractions that are not made are not read
+            constexpr bool score = Order::score(ahead % NOPS);
+            constexpr bool wanted = ahead < NOPS ? (score ? HAS_NEXT : HAS_PREV) : !DRAIN && (HAS_NEXT || !score);
             if constexpr (qb == 0 && wanted) {
-                ring[(G0 + j + RING - 1) % RING] = fetch(IntC<j + RING - 1>{}, slot, nb_c);
+                ring[(G0 + pos + RING - 1) % RING] = fetch(IntC<pos + RING - 1>{}, slot, nb_c);
             }
             // ---- this slot's share of the sigmoid
             static_for<(k * LEN) / SLOTS, ((k + 1) * LEN) / SLOTS>([&](auto i_) {
@@ -853,6 +889,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     using F_ = IntC<0>;
 
     // ---- prologue: tiles 0 and 1 of the stream into the ring, tile 2 into registers
+    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0);   // one owner tile a workgroup
     {   // the first three tiles are requested back to back, so their latencies overlap
         load_tile();
         u32x4 a1[C::PER], a2[C::PER];
@@ -887,8 +924,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     constexpr auto reads_from = [](int first_slot) {
         int cnt = 0;
         for (int k = first_slot; k < SLOTS; k += QB) {
-            const int j = (k / QB + RING - 1) % NOPS;
-            cnt += (j < NA) ? 1 : 2;           // one 16-byte read, or two transposing 8-byte reads
+            cnt += Order::score((k / QB + RING - 1) % NOPS) ? 1 : 2;   // one 16-byte read, or two transposing 8-byte reads
         }
         return cnt;
     };
@@ -901,14 +937,29 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     static_assert(READS_AFTER <= 15 && STORE_AT < SLOTS, "more reads behind the tile store than the LDS counter can express");
     using StoreAt = IntC<STORE_AT>;
     using NoStore = IntC<-1>;
+    // A block whose P and dS are packed (and masked, in the last tile): what is done to them before the next step contracts them.
+    auto finish = [&](auto nb_c) {
+        constexpr int PAR = decltype(nb_c)::value & 1;
+        if constexpr (Mod::SIFTED) {
+            static_for<0, QB>([&](auto q_) {
+                constexpr int qb = decltype(q_)::value;
+                mod.template sift<qb, MODE != DQ, HAS2>(pbuf[PAR][qb], dsbuf[PAR][HAS2 ? qb : 0]);
+            });
+            mod.next_block();
+        }
+        if constexpr (Mod::SUMMED) mod.sum(dsbuf[PAR][0]);
+        if constexpr (Mod::SIFTED || Mod::SUMMED) __builtin_amdgcn_sched_barrier(0);
+    };
     auto tile_body = [&](auto slot_c) {            // from the second block of a tile through the first of the next
         constexpr int slot = decltype(slot_c)::value;
+        finish(IntC<0>{});
         static_for<1, NB>([&](auto nb_) {
             if constexpr (decltype(nb_)::value + 1 < NB) step(T_{}, T_{}, F_{}, nb_, slot_c, NoStore{}, 0);
             else step(T_{}, T_{}, F_{}, nb_, slot_c, StoreAt{}, (slot + 2) & (C::NBUF - 1));
         });
         asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(READS_AFTER) : "memory");
         if constexpr (!LOAD_EARLY) load_tile();
+        finish(IntC<1>{});
         step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0);
     };
     // P and dS of the streamed rows behind the valid length, in block nb of the last tile: exact zeros, as packed for the
@@ -936,9 +987,11 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         __builtin_amdgcn_sched_barrier(0);
     };
     int slot_rt = 0;                               // ring slot of the tile in hand
+    if constexpr (Mod::BIASED) mod.fill();
     for (;;) {
         // the tiles stored last are visible, and nobody reads the slot that is written next
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if constexpr (Mod::SUMMED) mod.clear();
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
@@ -954,12 +1007,16 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         }
         {
             const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if constexpr (Mod::BIASED) {
+                static_for<0, QB>([&](auto q_) { mod.template start<decltype(q_)::value>(sbuf[0][decltype(q_)::value]); });
+                mod.advance();
+            }
 #pragma unroll
             for (int ks = 0; ks < C::KS; ++ks) {
                 const bf16x8 a1 = lds_read_rows(rd1 + slot_rt * BN * LD1 + 16 * ks);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
-                    sbuf[0][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, xa[qb][ks], ks == 0 ? zero : sbuf[0][qb], 0, 0, 0);
+                    sbuf[0][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, xa[qb][ks], ks == 0 && !Mod::BIASED ? zero : sbuf[0][qb], 0, 0, 0);
                 if (HAS2) {
                     const bf16x8 a2 = lds_read_rows(rd2 + slot_rt * BN * LD2 + 16 * ks);
 #pragma unroll
@@ -970,7 +1027,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         }
         // operands 0 .. RING - 2 of the first step
         static_for<0, RING - 1>([&](auto J_) {
-            if constexpr (decltype(J_)::value < NA) ring[decltype(J_)::value % RING] = fetch(J_, DynInt{slot_rt}, IntC<0>{});
+            if constexpr (Order::score(decltype(J_)::value)) ring[decltype(J_)::value % RING] = fetch(J_, DynInt{slot_rt}, IntC<0>{});
         });
         step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0);
 
@@ -991,9 +1048,11 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         {
             const DynInt slot{slot_rt};
             mask_block(IntC<0>{});
+            finish(IntC<0>{});
             static_for<1, NB>([&](auto nb_) {
                 step(T_{}, IntC<(decltype(nb_)::value + 1 < NB) ? 1 : 0>{}, F_{}, nb_, slot, NoStore{}, 0);
                 mask_block(nb_);
+                finish(nb_);
             });
             const DynInt slot_next{(slot_rt + 1) & (C::NBUF - 1)};
             step(T_{}, F_{}, T_{}, IntC<0>{}, slot_next, NoStore{}, 0);
@@ -1023,6 +1082,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             }
         }
 
+        if constexpr (Mod::SUMMED) mod.close();
+
         // ---- epilogue: transposed fp32 accumulators -> bf16 rows.  Lane (c, g) holds owner row c of each block;
         // registers 4 q4 .. 4 q4 + 3 of output block mb hold head-dim columns out_col(mb, q4) + 4 g + 0..3 of the
         // layout the transposed operand was read with (plain: 32 mb + 8 q4).  The two lanes of a row (32 apart)
@@ -1030,7 +1091,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         // whole 16-byte chunks: a quarter of the store instructions and write requests of 8-byte stores.
         using TL_ACC0 = TrLayout<(MODE == FWD) ? C::LM2 : C::LM1>;      // FWD contracts V^T; DQ K^T; DKDV Q^T (acc0), dO^T (acc1)
         using TL_ACC1 = TrLayout<C::LM2>;
-        const float oscale = (MODE == FWD) ? 1.0f : p.scale * cb;       // dQ and dK carry the factor `scale`; their sums are over dS / cb
+        const float used = Mod::SIFTED ? mod.scale() : 1.0f;            // of the weights
+        const float oscale = used * ((MODE == FWD) ? 1.0f : p.scale * cb);   // dQ and dK carry the factor `scale`; their sums are over dS / cb
         auto chunk = [&](const f32x16 &a, const int pr, const float f) {   // columns of q4 = 2 pr + g
             const unsigned e0 = pack_bf16(a[8 * pr + 0] * f, a[8 * pr + 1] * f), e1 = pack_bf16(a[8 * pr + 2] * f, a[8 * pr + 3] * f);
             const unsigned o0 = pack_bf16(a[8 * pr + 4] * f, a[8 * pr + 5] * f), o1 = pack_bf16(a[8 * pr + 6] * f, a[8 * pr + 7] * f);
@@ -1059,7 +1121,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                     const u32x4 w0 = chunk(acc0[qb][mb], pr, oscale);
                     __builtin_amdgcn_raw_buffer_store_b128(ok ? w0 : z4, d0, off + 2 * TL_ACC0::out_col(mb, 2 * pr), qb * block_bytes, 0);
                     if (MODE == DKDV) {
-                        const u32x4 w1 = chunk(acc1[MODE == DKDV ? qb : 0][MODE == DKDV ? mb : 0], pr, 1.0f);
+                        const u32x4 w1 = chunk(acc1[MODE == DKDV ? qb : 0][MODE == DKDV ? mb : 0], pr, used);
                         __builtin_amdgcn_raw_buffer_store_b128(ok ? w1 : z4, d1, off + 2 * TL_ACC1::out_col(mb, 2 * pr), qb * block_bytes, 0);
                     }
                 }
@@ -1124,7 +1186,7 @@ __global__ void __launch_bounds__(NW * 64, OCC) sigattn_bwd_kernel(const Params 
 // Second stage of the bias gradient: db[z] = sum of the `per_seq` partials of sequence z, in a fixed order
 // (thread t takes partials t, t + 256, ...; then a tree in LDS), so the result is bitwise reproducible.
 // One workgroup per sequence.
-__global__ void __launch_bounds__(256) sigattn_db_reduce(const float *part, int per_seq, float *db) {
+static __global__ void __launch_bounds__(256) sigattn_db_reduce(const float *part, int per_seq, float *db) {
     __shared__ float s[256];
     const int z = blockIdx.x;
     float t = 0.f;

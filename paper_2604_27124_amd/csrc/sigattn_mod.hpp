@@ -1,0 +1,332 @@
+// Attention whose scores carry a learned relative position bias and whose weights go through dropout, on the kernels of
+// sigattn_kernels.hpp:
+//
+//   x_ij  = scale <q_i, k_j> + bias[z] + table[b_ij][h],   b_ij = buckets[clamp(j - i - q_start[z], -reach, reach) + reach]
+//   O_i   = sum_j m_ij P_ij v_j / keep,                    P = sigma(x),  m_ij in {0, 1} with share `keep` of ones
+//   dS_ij = P_ij (1 - P_ij) m_ij dP_ij / keep,             dV_j = sum_i m_ij P_ij dO_i / keep
+//   dtable[b][h] = sum over z, i, j with b_ij = b of dS_ij
+//
+// The bias depends on j - i alone.  Streamed rows pass an owner row in order, so the values that the score tiles of an owner
+// tile start from (the accumulators of the score contraction: no vector instruction adds them) are a window of one vector
+// over the distances, which moves on by 64 entries a tile.  It lives in a ring in LDS; a tile's new entries are looked up
+// (bucket, then table) a tile ahead of each other and stored with the tile.  Any reach costs the same.
+#pragma once
+#include "sigattn_kernels.hpp"
+
+namespace sigattn {
+namespace mod {
+
+typedef unsigned long long u64;
+
+// The far sums of a sequence of many blocks, and everything else about dS, are of dS / c (c = 2^(-bias log2 e), as in run_pass) and without
+// 1 / keep: the kernel that adds up the rows applies both.
+struct Extra {                       // what the calls take besides Params
+    const bf16_t *table;             // [num_buckets][H]
+    const int32_t *buckets;          // [2 reach + 1]
+    const int32_t *q_start;          // [B], or null for zeros: position of query row 0 among the keys
+    int num_buckets, reach;
+    const u64 *rng;                  // {seed, offset}
+    unsigned keep;                   // of 65536 weights, those that stay
+    float inv_keep;                  // 65536 / keep
+    float *part;                     // sums of dS by distance, see RowSums below
+    float *by_distance;
+};
+
+// ---- sums of dS by distance
+//
+// For 32 queries [32 ob, 32 ob + 32) and 32 keys [32 b, 32 b + 32) the distances j - i - q_start are 32 (b - ob) - q_start + [-31, 31].
+// Blocks wholly at or beyond +-reach belong to one bucket each and are summed as they are; of the others ("near") every
+// distance is summed on its own.  For each ob a row of partial sums: entry 32 (k - first) + c, k = b - ob, is that of distance
+// 32 k - q_start - 31 + c; behind the entries of all near blocks and one more the sums of the two far sides.
+struct RowSums {
+    int first, last;                 // near block diagonals k of a sequence: [first, last]
+    __host__ __device__ static int down(int a) { return a >> 5; }                                  // a / 32, rounded down
+    __device__ __forceinline__ RowSums(int reach, int start, int row_blocks) {
+        first = down(start - reach - 31) + 1;                  // smallest k with 32 k - start + 31 > -reach
+        last = -down(-(start + reach + 31)) - 1;               // largest k with 32 k - start - 31 < reach
+        const int low = 1 - row_blocks;                        // no smaller k exists
+        first = first < low ? low : first;
+    }
+    // entries of a row (a multiple of 32), for any q_start
+    __host__ __device__ static int entries(int reach, int L_q, int L_k) {
+        const int near = (2 * reach + 62) / 32 + 2, all = (L_q + 31) / 32 + 2 * ((L_k + 63) / 64);
+        return 32 * ((near < all ? near : all) + 1);
+    }
+};
+constexpr int FAR = 32;              // floats behind the entries of a row: [0] the far side below, [1] the one above
+
+// What one pass adds to a kernel.  BIASED: the position bias; SIFTED: dropout; SUMMED: sums of dS by distance (DQ).
+template <int MODE, int QB, int NW, bool BIAS, bool DROP, bool SUM>
+struct Mods {
+    static constexpr bool BIASED = BIAS, SIFTED = DROP, SUMMED = SUM;
+    static constexpr int BM = 32 * QB * NW, THREADS = 64 * NW;
+    static constexpr int RING = 512, MIRROR = 32;              // floats; what is read past the end is kept there again
+    static constexpr int WINDOW = 160;                         // floats a wave: two halves of 64, 92 apart (disjoint banks)
+    static_assert(BM + 160 <= RING, "live entries: an owner tile, the tile in hand and two more");
+    static_assert(!SUM || (MODE == DQ && QB == 1), "sums ride on the dQ pass");
+
+    const Params &p;
+    const Extra &x;
+    float *const ring;                                         // LDS [RING + MIRROR]
+    float *const windows;                                      // LDS [NW][WINDOW]
+    int h, n, ns, m0, start_pos;
+    int wave, lane;
+
+    // bias
+    unsigned at;                                               // byte in the ring of this lane's first entry, owner block 0
+    int next_x, next_pos;                                      // chunk that is looked up next: distance of its entry 0, ring position
+    int bucket;
+    float value;
+
+    // dropout
+    unsigned key0, key1, c3, c2, row, group;                   // row, group: counter words of owner block 0, this block
+    unsigned ph[DROP ? QB : 1][4], stays[DROP ? QB : 1];
+
+    // sums
+    float *out_row;
+    int k, first, last, entries;
+    bool active, open_window;
+    f32x4 far;
+    float below;
+
+    __device__ __forceinline__ Mods(const Params &p_, const Extra &x_, float *ring_, float *windows_) : p(p_), x(x_), ring(ring_), windows(windows_) {}
+
+    // ---------------------------------------------------------------- bias
+    // Distance (streamed - owner) `d` -> value; 0 for distances that no valid pair has, which padding alone reads.
+    __device__ __forceinline__ int bucket_at(const int d) const {
+        int t = MODE == DKDV ? -d - start_pos : d - start_pos;
+        t = t < -x.reach ? -x.reach : (t > x.reach ? x.reach : t);
+        return x.buckets[t + x.reach];
+    }
+    __device__ __forceinline__ float value_of(const int b, const int d) const {
+        const int c = b < 0 ? 0 : (b >= x.num_buckets ? x.num_buckets - 1 : b);
+        const float v = (float)x.table[(size_t)c * p.H + h] * -1.4426950408889634f;
+        return d > -n && d < ns ? v : 0.f;
+    }
+
+    __device__ __forceinline__ void open(const int z, const int h_, const int n_, const int ns_, const int m0_) {
+        h = h_; n = n_; ns = ns_; m0 = m0_;
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int c = lane & 31, g = lane >> 5;
+        if constexpr (BIAS) {
+            int s = x.q_start ? x.q_start[z] : 0;
+            s = s < -(1 << 29) ? -(1 << 29) : (s > (1 << 29) ? (1 << 29) : s);
+            start_pos = __builtin_amdgcn_readfirstlane(s);
+            at = 4u * (unsigned)((BM - 32 * QB * wave - c + 4 * g) & (RING - 1));
+            next_x = -m0;
+            next_pos = BM & (RING - 1);
+            bucket = bucket_at(next_x + lane);
+        }
+        if constexpr (DROP) {
+            const u64 seed = x.rng[0], offset = x.rng[1];
+            key0 = __builtin_amdgcn_readfirstlane((unsigned)seed);
+            key1 = __builtin_amdgcn_readfirstlane((unsigned)(seed >> 32));
+            c3 = __builtin_amdgcn_readfirstlane((unsigned)offset);
+            c2 = __builtin_amdgcn_readfirstlane((unsigned)z * (unsigned)p.H + (unsigned)h);
+            if constexpr (MODE == DKDV) { row = c; group = 2 * (m0 / 32 + wave) + g; }
+            else { row = m0 + 32 * QB * wave + c; group = g; }
+        }
+        if constexpr (SUM) {
+            const int ob = m0 / 32 + wave, blocks = (p.N + 31) / 32;
+            const RowSums r(x.reach, start_pos, blocks);
+            first = r.first; last = r.last;
+            entries = RowSums::entries(x.reach, p.N, p.N_str);
+            k = -ob;                                           // diagonal of key block 0
+            active = 32 * ob < n;
+            open_window = false;
+            out_row = x.part + (((size_t)z * p.H + h) * blocks + ob) * (size_t)(entries + FAR);
+            far = f32x4{0.f, 0.f, 0.f, 0.f};
+            below = 0.f;
+        }
+    }
+    // The entries of the first two tiles and of the owner tile in front of them.
+    __device__ __forceinline__ void fill() {
+        for (int e = threadIdx.x; e < BM + 128; e += THREADS) {
+            const int d = e - BM - m0;
+            const float v = value_of(bucket_at(d), d);
+            ring[e] = v;
+            if (e < MIRROR) ring[RING + e] = v;
+        }
+    }
+    // With a tile's loads: the values of its 64 entries, and the buckets of the next one's.  (Every wave does the same.)
+    __device__ __forceinline__ void request() {
+        value = value_of(bucket, next_x + lane);
+        next_x += 64;
+        bucket = bucket_at(next_x + lane);
+    }
+    // With a tile's stores.  The first two tiles are in the ring already.
+    __device__ __forceinline__ void store() {
+        const int pos = (next_pos + 128) & (RING - 1);
+        ring[pos + lane] = value;
+        if (pos == 0 && lane < MIRROR) ring[RING + lane] = value;
+        next_pos = (next_pos + 64) & (RING - 1);
+    }
+    // What the score tile of owner block qb starts from, next streamed block.
+    template <int qb>
+    __device__ __forceinline__ void start(f32x16 &s) const {
+        const unsigned from = (at - 128u * qb) & (4 * RING - 1);
+        const float *const r = reinterpret_cast<const float *>(reinterpret_cast<const char *>(ring) + from);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = r[8 * (i / 4) + i % 4];
+    }
+    __device__ __forceinline__ void advance() { at = (at + 128u) & (4 * RING - 1); }
+
+    // ---------------------------------------------------------------- dropout
+    __device__ __forceinline__ float scale() const { return x.inv_keep; }
+
+    __device__ __forceinline__ static unsigned majority(unsigned a, unsigned b, unsigned c) { return (a & b) | (c & (a | b)); }
+
+    // Part `item` of the generator of owner block qb: seven rounds of Philox4x32 (Salmon, Moraes, Dror, Shaw 2011), then the 16
+    // decisions of a lane.  Decision t takes bits t and t + 8 of each of the four words as its byte; its 16-bit number u is that
+    // byte and, below it and bit-reversed, the byte of decision t ^ 16.  It stays where u + keep carries out of 16 bits, and
+    // the carries of all decisions run through the bits of `keep` at once, one majority a bit.
+    template <int qb, int item>
+    __device__ __forceinline__ void generate() {
+        unsigned (&c)[4] = ph[qb];
+        if constexpr (item == 0) {
+            c[0] = row + (MODE == DKDV ? 0 : 32 * qb);
+            c[1] = group + (MODE == DKDV ? 2 * qb : 0);
+            c[2] = c2;
+            c[3] = c3;
+        }
+        if constexpr (item < 7) {
+            const u64 a = (u64)0xD2511F53u * c[0], b = (u64)0xCD9E8D57u * c[2];
+            const unsigned k0 = key0 + item * 0x9E3779B9u, k1 = key1 + item * 0xBB67AE85u;
+            const unsigned n0 = (unsigned)(b >> 32) ^ c[1] ^ k0, n2 = (unsigned)(a >> 32) ^ c[3] ^ k1;
+            c[0] = n0; c[1] = (unsigned)b; c[2] = n2; c[3] = (unsigned)a;
+        } else {
+            unsigned m = 0;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const unsigned bit = 0u - ((x.keep >> s) & 1u);
+                m = majority(c[(7 - s) / 2] >> (8 * ((7 - s) % 2)), m, bit);
+            }
+            m = __builtin_amdgcn_alignbit(m, m, 16);
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const unsigned bit = 0u - ((x.keep >> (8 + s)) & 1u);
+                m = majority(c[s / 2] >> (8 * (s % 2)), m, bit);
+            }
+            stays[qb] = MODE == DKDV ? turned(m) : m;
+        }
+    }
+    // Bits w and 16 + w (w < 8) of lane (c, g) are the decisions of query c for keys 8 (w / 2) + 4 g + 2 (w % 2) + {0, 1}; with
+    // keys and queries exchanged in the result.  The words of both halves of the wave are joined into rows of 32 bits, and
+    // each of five steps exchanges one bit of the lane's number with the bit of the position that stands for the same bit of
+    // the other tensor's row.
+    template <int STRIDE>
+    __device__ __forceinline__ static unsigned exchange(const unsigned own, const unsigned other, const bool upper) {
+        constexpr unsigned LOW = STRIDE == 1 ? 0x55555555u : STRIDE == 2 ? 0x33333333u : STRIDE == 4 ? 0x0F0F0F0Fu : STRIDE == 8 ? 0x00FF00FFu : 0x0000FFFFu;
+        const unsigned moved = __builtin_amdgcn_alignbit(other, other, upper ? STRIDE : 32 - STRIDE);
+        const unsigned mine = upper ? ~LOW : LOW;
+        return (own & mine) | (moved & ~mine);
+    }
+    template <int CTRL>
+    __device__ __forceinline__ static unsigned dpp(const unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+    __device__ __forceinline__ unsigned turned(unsigned m) const {
+        const int g = lane >> 5;
+        m = (m & 0x00FF00FFu) << (8 * g);
+        const auto halves = __builtin_amdgcn_permlane32_swap(m, m, false, false);     // {lower half's words, upper half's} in every lane
+        unsigned v = halves[0] | halves[1];
+        v = exchange<16>(v, dpp<0xB1>(v), lane & 1);                                   // quad_perm 1, 0, 3, 2
+        v = exchange<1>(v, dpp<0x4E>(v), lane & 2);                                    // quad_perm 2, 3, 0, 1
+        v = exchange<8>(v, dpp<0x1B>(dpp<0x141>(v)), lane & 4);                        // half mirror, then quad_perm 3, 2, 1, 0
+        v = exchange<2>(v, dpp<0x128>(v), lane & 8);                                   // rotation of a row of 16 by 8
+        const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = exchange<4>(v, lane & 16 ? rows[0] : rows[1], lane & 16);
+        return v >> (8 * g);
+    }
+
+    // The share of slot K of SLOTS of a step.
+    template <int K, int SLOTS>
+    __device__ __forceinline__ void slot() {
+        static_for<(K * 8 * QB) / SLOTS, ((K + 1) * 8 * QB) / SLOTS>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            generate<i / 8, i % 8>();
+        });
+    }
+    template <int qb, bool WEIGHTS, bool DS>
+    __device__ __forceinline__ void sift(u32x4 (&w)[2], u32x4 (&ds)[2]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const s16x2 both = __builtin_bit_cast(s16x2, stays[qb] << (15 - i));
+            const unsigned keep = __builtin_bit_cast(unsigned, (s16x2)(both >> 15));
+            if (WEIGHTS) w[i / 4][i % 4] &= keep;
+            if (DS) ds[i / 4][i % 4] &= keep;
+        }
+    }
+    __device__ __forceinline__ void next_block() {
+        if (MODE == DKDV) row += 32;
+        else group += 2;
+    }
+
+    // ---------------------------------------------------------------- sums of dS
+    // Near blocks: each half of a wave adds its values into a window of its own over the 63 distances of the block, in LDS.
+    // The lanes of a half hold different distances in every instruction and a wave's LDS operations complete in order, so
+    // the order of every sum is fixed.  Then the 32 distances that no later block reaches go out and the window moves on.
+    // The summands are the bf16 values that also feed dQ.
+    __device__ __forceinline__ void clear() {
+        float *const w = windows + wave * WINDOW;
+        for (int e = lane; e < WINDOW; e += 64) w[e] = 0.f;
+    }
+    __device__ __forceinline__ void flush() {
+        const int c = lane & 31, g = lane >> 5;
+        float *const w = windows + wave * WINDOW + 92 * g;
+        const float done = w[c], rest = w[c + 32];
+        w[c] = rest;
+        w[c + 32] = 0.f;
+        const float other = __shfl_xor(done, 32, 64);
+        if (g == 0) out_row[32 * (k - first) + c] = done + other;
+    }
+    __device__ __forceinline__ void sum(const u32x4 (&packed)[2]) {
+        if (!active) return;                                   // uniform
+        const int c = lane & 31, g = lane >> 5;
+        u32x4 ds[2] = {packed[0], packed[1]};
+        if (n - m0 - 32 * wave < 32) {                         // rows behind the valid queries: a key of Inf would make them NaN
+            const unsigned ok = m0 + 32 * wave + c < n ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ds[i / 4][i % 4] &= ok;
+        }
+        if (k >= first && k <= last) {
+            if (!open_window) { below = far[0]; far = f32x4{0.f, 0.f, 0.f, 0.f}; open_window = true; }
+            float *const w = windows + wave * WINDOW + 92 * g + 31 - c + 4 * g;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const unsigned v = ds[i / 4][i % 4];
+                const int r = 8 * (i / 2) + 2 * (i % 2);
+                __hip_atomic_fetch_add(w + r, __builtin_bit_cast(float, v << 16), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                __hip_atomic_fetch_add(w + r + 1, __builtin_bit_cast(float, v & 0xFFFF0000u), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+            }
+            flush();
+        } else {
+            if (k > last && open_window) { flush(); open_window = false; }
+            bf16x8 ones;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ones[i] = (bf16_t)1.0f;
+            far = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[0]), far, 0, 0, 0);
+            far = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[1]), far, 0, 0, 0);
+        }
+        ++k;
+    }
+    // Behind the last block: what is left in the window, and the far sums.
+    __device__ __forceinline__ void close() {
+        if (!active) return;
+        if (open_window) flush();
+        const bool all_below = k <= first;                     // not one block was near, or beyond
+        float v = lane < 16 ? far[0] : 0.f;
+        float u = lane < 16 ? below : 0.f;
+#pragma unroll
+        for (int off = 8; off >= 1; off >>= 1) {
+            v += __shfl_xor(v, off, 64);
+            u += __shfl_xor(u, off, 64);
+        }
+        if (lane == 0) {
+            out_row[entries] = all_below ? v : u;
+            out_row[entries + 1] = all_below ? 0.f : v;
+        }
+    }
+};
+
+}  // namespace mod
+}  // namespace sigattn

@@ -1,0 +1,278 @@
+// Host side of the calls with a relative position bias and with dropout (include/sigmoid_attn.h), and the kernels that add up the
+// gradient of the bias table.
+#include "sigattn_mod_launch.hpp"
+
+#include <cmath>
+
+using namespace sigattn;
+using mod::Extra;
+using mod::RowSums;
+
+namespace {
+
+constexpr int MOST_REACH = 1 << 24, MOST_BUCKETS = 1 << 16, MOST_ROWS = 1 << 29;
+
+struct Lengths {
+    const int32_t *q, *k, *start;    // [B]; start may be null
+    const float *bias;
+    int L_q, L_k, H, B;
+};
+
+__device__ __forceinline__ int clamped(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+
+__device__ __forceinline__ int start_of(const Lengths &l, int z) { return l.start ? clamped(l.start[z], -(1 << 29), 1 << 29) : 0; }
+
+// Group s of `groups` adds up the rows of sequences s, s + groups, ...: [group][H][entries + FAR].  A workgroup takes 32 entries of a
+// head; its eight groups of 32 lanes take the rows of a sequence in turn.  Fixed order, no atomics.
+__global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const Extra x, const int groups) {
+    __shared__ float s[8][32];
+    const int entries = RowSums::entries(x.reach, l.L_q, l.L_k), chunks = entries / 32 + 1;
+    const int chunk = blockIdx.x % chunks, rest = blockIdx.x / chunks, h = rest % l.H, group = rest / l.H;
+    const int c = threadIdx.x & 31, mine = threadIdx.x >> 5;
+    const int blocks = (l.L_q + 31) / 32;
+    const bool far = chunk == chunks - 1;
+    float total = 0.f;
+    for (int z = group; z < l.B; z += groups) {
+        const int nq = clamped(l.q[z], 0, l.L_q), ns = clamped(l.k[z], 0, l.L_k);
+        if (nq == 0 || ns == 0) continue;
+        const RowSums r(x.reach, start_of(l, z), blocks);
+        const int k = r.first + chunk, key_blocks = 2 * ((ns + 63) / 64);
+        const float *const rows = x.part + ((size_t)z * l.H + h) * blocks * (size_t)(entries + mod::FAR) + 32 * chunk + c;
+        float t = 0.f;
+        for (int ob = mine; 32 * ob < nq; ob += 8) {
+            // written: what a near block sent out, and what the last near block left behind
+            const bool here = k <= r.last && k + ob >= 0 && k + ob < key_blocks;
+            const bool left = chunk > 0 && k - 1 <= r.last && k - 1 + ob >= 0 && k - 1 + ob < key_blocks;
+            if (far ? c < 2 : here || left) t += rows[ob * (size_t)(entries + mod::FAR)];
+        }
+        const float cb = __builtin_amdgcn_exp2f(__builtin_fminf(__builtin_fmaxf(-l.bias[z] * 1.4426950408889634f, -126.0f), 126.0f));
+        total += t * (cb * x.inv_keep);
+    }
+    s[mine][c] = total;
+    __syncthreads();
+    if (mine == 0) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t += s[i][c];
+        x.by_distance[((size_t)group * l.H + h) * (entries + mod::FAR) + 32 * chunk + c] = t;
+    }
+}
+
+// dtable[b][h]: a wave for a bucket, over the distances of every group.
+__global__ void __launch_bounds__(256) sigattn_rel_table(const Lengths l, const Extra x, const int groups, bf16_t *dtable) {
+    const int wide = (x.num_buckets + 3) / 4;
+    const int h = blockIdx.x / wide, b = blockIdx.x % wide * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (b >= x.num_buckets) return;
+    const int entries = RowSums::entries(x.reach, l.L_q, l.L_k);
+    auto bucket = [&](int t) { return clamped(x.buckets[clamped(t, -x.reach, x.reach) + x.reach], 0, x.num_buckets - 1); };
+    float total = 0.f;
+    for (int g = 0; g < groups; ++g) {
+        const int start = start_of(l, g);                      // groups share a start only if there is none
+        const RowSums r(x.reach, start, (l.L_q + 31) / 32);
+        const float *const d = x.by_distance + ((size_t)g * l.H + h) * (entries + mod::FAR);
+        for (int e = lane; e < entries; e += 64)
+            if (bucket(32 * r.first - start - 31 + e) == b) total += d[e];
+        if (lane < 2 && bucket(lane == 0 ? -x.reach : x.reach) == b) total += d[entries + lane];
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off, 64);
+    if (lane == 0) dtable[(size_t)b * l.H + h] = (bf16_t)total;
+}
+
+bool aligned(const void *p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+struct Bias {
+    const void *table;
+    const int32_t *buckets;
+    int num_buckets, reach;
+    const int32_t *q_start;
+};
+struct Drop {
+    float p;
+    const uint64_t *rng;
+};
+
+int check(const void *q, const void *k, const void *v, const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+          const Bias *rel, const Drop *drop, int B, int L_q, int L_k, int H, int d) {
+    if (!q || !k || !v || !seqlens_q || !seqlens_k || !bias || !std::isfinite(scale)) return SIGATTN_ERR_INVALID_ARG;
+    if (rel && (!rel->table || !rel->buckets || rel->num_buckets <= 0 || rel->reach < 0)) return SIGATTN_ERR_INVALID_ARG;
+    if (drop && (!drop->rng || !(drop->p >= 0.0f && drop->p < 1.0f))) return SIGATTN_ERR_INVALID_ARG;
+    if (int e = check_shape(B, L_q, H, d)) return e;
+    if (int e = check_shape(B, L_k, H, d)) return e;
+    if (L_q > MOST_ROWS || L_k > MOST_ROWS) return SIGATTN_ERR_TOO_LARGE;
+    if (rel && (rel->reach > MOST_REACH || rel->num_buckets > MOST_BUCKETS)) return SIGATTN_ERR_TOO_LARGE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned(seqlens_q, 4) || !aligned(seqlens_k, 4) || !aligned(bias, 4)) return SIGATTN_ERR_MISALIGNED;
+    if (rel && (!aligned(rel->table, 2) || !aligned(rel->buckets, 4) || !aligned(rel->q_start, 4))) return SIGATTN_ERR_MISALIGNED;
+    if (drop && !aligned(drop->rng, 8)) return SIGATTN_ERR_MISALIGNED;
+    return SIGATTN_OK;
+}
+
+// Of 65536 weights, those that stay: at least one; 65536 of them is no dropout.
+unsigned kept(float p) {
+    const unsigned k = (unsigned)std::floor((1.0 - (double)p) * 65536.0 + 0.5);
+    return k < 1 ? 1 : k;
+}
+
+Extra extra(const Bias *rel, const Drop *drop) {
+    Extra x{};
+    x.inv_keep = 1.0f;
+    if (rel) {
+        x.table = static_cast<const bf16_t *>(rel->table);
+        x.buckets = rel->buckets;
+        x.q_start = rel->q_start;
+        x.num_buckets = rel->num_buckets;
+        x.reach = rel->reach;
+    }
+    if (drop) {
+        x.rng = reinterpret_cast<const mod::u64 *>(drop->rng);
+        x.keep = kept(drop->p);
+        x.inv_keep = (float)(65536.0 / x.keep);
+    }
+    return x;
+}
+
+int forward(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
+            const Bias *rel, const Drop *drop, int B, int L_q, int L_k, int H, int d, void *stream) {
+    if (!o) return SIGATTN_ERR_INVALID_ARG;
+    if (int e = check(q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, B, L_q, L_k, H, d)) return e;
+    if (!aligned16(o)) return SIGATTN_ERR_MISALIGNED;
+    if (drop && kept(drop->p) == 65536) drop = nullptr;
+    if (!rel && !drop) return sigmoid_attn_cross_fwd(q, k, v, o, seqlens_q, seqlens_k, bias, scale, B, L_q, L_k, H, d, stream);
+    Params p{};
+    p.q = static_cast<const bf16_t *>(q);
+    p.k = static_cast<const bf16_t *>(k);
+    p.v = static_cast<const bf16_t *>(v);
+    p.out0 = static_cast<bf16_t *>(o);
+    p.seqlens = seqlens_q; p.N = L_q;
+    p.seqlens_str = seqlens_k; p.N_str = L_k;
+    p.bias = bias; p.scale = scale; p.B = B; p.H = H;
+    const Extra x = extra(rel, drop);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return rel && drop ? mod::fwd_rel_dropout(p, x, d, s) : rel ? mod::fwd_rel(p, x, d, s) : mod::fwd_dropout(p, x, d, s);
+}
+
+// The workspace of a backward call with a bias table: a row of sums for every 32 queries, and their sums by group.
+size_t row_floats(int B, int L_q, int L_k, int H, int reach) {
+    return (size_t)B * H * (((size_t)L_q + 31) / 32) * (RowSums::entries(reach, L_q, L_k) + mod::FAR);
+}
+size_t group_floats(int B, int L_q, int L_k, int H, int reach) { return (size_t)B * H * (RowSums::entries(reach, L_q, L_k) + mod::FAR); }
+
+size_t rel_bytes(int B, int L_q, int L_k, int H, int d, int reach) {
+    if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK) return 0;
+    if (L_q > MOST_ROWS || L_k > MOST_ROWS || reach < 0 || reach > MOST_REACH) return 0;
+    return (row_floats(B, L_q, L_k, H, reach) + group_floats(B, L_q, L_k, H, reach)) * sizeof(float);
+}
+
+int backward(const void *q, const void *k, const void *v, const void *d_o, void *dq, void *dk, void *dv, void *dtable,
+             const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale, const Bias *rel, const Drop *drop,
+             int B, int L_q, int L_k, int H, int d, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!d_o || !dq || !dk || !dv || (rel && !dtable)) return SIGATTN_ERR_INVALID_ARG;
+    if (int e = check(q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, B, L_q, L_k, H, d)) return e;
+    if (!aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned(dtable, 2)) return SIGATTN_ERR_MISALIGNED;
+    if (rel && (!workspace || workspace_bytes < rel_bytes(B, L_q, L_k, H, d, rel->reach))) return SIGATTN_ERR_WORKSPACE;
+    if (rel && !aligned16(workspace)) return SIGATTN_ERR_MISALIGNED;
+    if (drop && kept(drop->p) == 65536) drop = nullptr;
+    if (!rel && !drop) return sigmoid_attn_cross_bwd(q, k, v, d_o, dq, dk, dv, seqlens_q, seqlens_k, bias, scale, B, L_q, L_k, H, d, stream);
+    Params p{};
+    p.q = static_cast<const bf16_t *>(q);
+    p.k = static_cast<const bf16_t *>(k);
+    p.v = static_cast<const bf16_t *>(v);
+    p.d_o = static_cast<const bf16_t *>(d_o);
+    p.bias = bias; p.scale = scale; p.B = B; p.H = H;
+    Params pk = p, pq = p;
+    pk.seqlens = seqlens_k; pk.N = L_k;
+    pk.seqlens_str = seqlens_q; pk.N_str = L_q;
+    pk.out0 = static_cast<bf16_t *>(dk);
+    pk.out1 = static_cast<bf16_t *>(dv);
+    pq.seqlens = seqlens_q; pq.N = L_q;
+    pq.seqlens_str = seqlens_k; pq.N_str = L_k;
+    pq.out0 = static_cast<bf16_t *>(dq);
+    Extra x = extra(rel, drop);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!rel) return mod::bwd_dropout(pk, pq, x, d, s);
+
+    const int entries = RowSums::entries(rel->reach, L_q, L_k), groups = rel->q_start || B < 16 ? B : 16;
+    const long long row_wgs = (long long)groups * H * (entries / 32 + 1), table_wgs = (long long)H * ((rel->num_buckets + 3) / 4);
+    if (row_wgs > 2147483647LL || table_wgs > 2147483647LL) return SIGATTN_ERR_TOO_LARGE;
+    x.part = static_cast<float *>(workspace);
+    x.by_distance = x.part + row_floats(B, L_q, L_k, H, rel->reach);
+    if (int e = drop ? mod::bwd_rel_dropout(pk, pq, x, d, s) : mod::bwd_rel(pk, pq, x, d, s)) return e;
+    const Lengths l{seqlens_q, seqlens_k, rel->q_start, bias, L_q, L_k, H, B};
+    if (int e = enqueue(sigattn_rel_rows, row_wgs, 256, 0, s, l, x, groups)) return e;
+    return enqueue(sigattn_rel_table, table_wgs, 256, 0, s, l, x, groups, static_cast<bf16_t *>(dtable));
+}
+
+}  // namespace
+
+extern "C" {
+
+int sigmoid_attn_rel_buckets(int32_t *buckets, int num_buckets, int reach) {
+    if (!buckets || num_buckets <= 0 || reach < 0) return SIGATTN_ERR_INVALID_ARG;
+    if (num_buckets > MOST_BUCKETS || reach > MOST_REACH) return SIGATTN_ERR_TOO_LARGE;
+    const int half = num_buckets / 2 > 1 ? num_buckets / 2 : 1, exact = half / 2 > 1 ? half / 2 : 1;
+    for (int t = -reach; t <= reach; ++t) {
+        const int a = t < 0 ? -t : t;
+        int b;
+        if (num_buckets >= 2 * reach + 1) {
+            b = t + reach;
+        } else {
+            b = a;
+            if (a >= exact)
+                b = exact + (int)(std::log((double)a / exact) / std::log((double)(reach > exact ? reach : exact + 1) / exact) * (half - exact));
+            if (b > half - 1) b = half - 1;
+            if (t > 0) b += half;
+            if (b > num_buckets - 1) b = num_buckets - 1;
+        }
+        buckets[t + reach] = b;
+    }
+    return SIGATTN_OK;
+}
+
+int sigmoid_attn_rel_fwd(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k,
+                         const float *bias, float scale, const void *table, const int32_t *buckets, int num_buckets, int reach,
+                         const int32_t *q_start, int B, int L_q, int L_k, int H, int d, void *stream) {
+    const Bias rel{table, buckets, num_buckets, reach, q_start};
+    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, &rel, nullptr, B, L_q, L_k, H, d, stream);
+}
+
+int sigmoid_attn_dropout_fwd(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k,
+                             const float *bias, float scale, float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream) {
+    const Drop drop{p, rng};
+    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, nullptr, &drop, B, L_q, L_k, H, d, stream);
+}
+
+int sigmoid_attn_rel_dropout_fwd(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k,
+                                 const float *bias, float scale, const void *table, const int32_t *buckets, int num_buckets, int reach,
+                                 const int32_t *q_start, float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream) {
+    const Bias rel{table, buckets, num_buckets, reach, q_start};
+    const Drop drop{p, rng};
+    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, &rel, &drop, B, L_q, L_k, H, d, stream);
+}
+
+size_t sigmoid_attn_rel_bwd_workspace_bytes(int B, int L_q, int L_k, int H, int d, int reach) { return rel_bytes(B, L_q, L_k, H, d, reach); }
+
+int sigmoid_attn_rel_bwd(const void *q, const void *k, const void *v, const void *d_o, void *dq, void *dk, void *dv, void *dtable,
+                         const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale, const void *table,
+                         const int32_t *buckets, int num_buckets, int reach, const int32_t *q_start, int B, int L_q, int L_k, int H, int d,
+                         void *workspace, size_t workspace_bytes, void *stream) {
+    const Bias rel{table, buckets, num_buckets, reach, q_start};
+    return backward(q, k, v, d_o, dq, dk, dv, dtable, seqlens_q, seqlens_k, bias, scale, &rel, nullptr, B, L_q, L_k, H, d, workspace, workspace_bytes, stream);
+}
+
+int sigmoid_attn_dropout_bwd(const void *q, const void *k, const void *v, const void *d_o, void *dq, void *dk, void *dv,
+                             const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale, float p, const uint64_t *rng,
+                             int B, int L_q, int L_k, int H, int d, void *stream) {
+    const Drop drop{p, rng};
+    return backward(q, k, v, d_o, dq, dk, dv, nullptr, seqlens_q, seqlens_k, bias, scale, nullptr, &drop, B, L_q, L_k, H, d, nullptr, 0, stream);
+}
+
+int sigmoid_attn_rel_dropout_bwd(const void *q, const void *k, const void *v, const void *d_o, void *dq, void *dk, void *dv, void *dtable,
+                                 const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale, const void *table,
+                                 const int32_t *buckets, int num_buckets, int reach, const int32_t *q_start, float p, const uint64_t *rng,
+                                 int B, int L_q, int L_k, int H, int d, void *workspace, size_t workspace_bytes, void *stream) {
+    const Bias rel{table, buckets, num_buckets, reach, q_start};
+    const Drop drop{p, rng};
+    return backward(q, k, v, d_o, dq, dk, dv, dtable, seqlens_q, seqlens_k, bias, scale, &rel, &drop, B, L_q, L_k, H, d, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,94 @@
+// The kernels of sigattn_mod.hpp and their launches.  Each combination (bias, dropout, both) is a translation unit of its own.
+#pragma once
+#include "sigattn_host.hpp"
+#include "sigattn_mod.hpp"
+
+namespace sigattn {
+namespace mod {
+
+template <int NW>
+struct Scratch {
+    union {                                                    // the windows are cleared behind the first barrier after the mapping
+        MapScratch map;
+        float windows[NW * 160];
+    };
+    float ring[512 + 32];
+};
+
+template <int MODE, int D, int QB, int NW, int LD1, int LD2, int OCC, int RING, bool BIAS, bool DROP>
+__global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod(const Params p, const Extra x) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ Scratch<NW> s;
+    using C = Cfg<MODE, D, QB, NW, 64, LD1, LD2, RING>;
+    using M = Mods<MODE, QB, NW, BIAS, DROP, BIAS && MODE == DQ>;
+    run_pass<MODE, D, QB, NW, 64, LD1, LD2, RING, false, M>(p, map_work<C::BM, C::THREADS>(p, blockIdx.x, s.map), smem, nullptr, M(p, x, s.ring, s.windows));
+}
+
+// d = 64: both passes of the backward in one launch, as in sigattn_bwd_kernel.
+template <int D, int NW, int LD, int OCC, int RING_KV, int RING_Q, bool BIAS, bool DROP>
+__global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod_bwd(const Params kv, const Params q, const Extra x, const int q_first, const int first_tiles) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ Scratch<NW> s;
+    using C = Cfg<DKDV, D, 1, NW, 64, LD, LD, RING_KV>;
+    using MK = Mods<DKDV, 1, NW, BIAS, DROP, false>;
+    using MQ = Mods<DQ, 1, NW, BIAS, DROP, BIAS>;
+    const int id = blockIdx.x;
+    Work w;
+    bool is_kv;
+    if (kv.in_order) {
+        const int t_kv = owner_tiles<C::BM>(kv), t_q = owner_tiles<C::BM>(q);
+        int tile;
+        batch_order_tile(id, kv.H, t_kv + t_q, w.z, w.h, tile);
+        is_kv = tile < t_kv;
+        w.n = owner_length(is_kv ? kv : q, w.z);
+        w.m0 = (is_kv ? tile : tile - t_kv) * C::BM;
+        w.count = 1;
+        w.share = w.shares = 0;
+    } else {
+        is_kv = (id < first_tiles) != (q_first != 0);
+        const int rest = id < first_tiles ? id : id - first_tiles;
+        w = is_kv ? map_work<C::BM, C::THREADS>(kv, rest, s.map) : map_work<C::BM, C::THREADS>(q, rest, s.map);
+    }
+    if (is_kv) run_pass<DKDV, D, 1, NW, 64, LD, LD, RING_KV, false, MK>(kv, w, smem, nullptr, MK(kv, x, s.ring, s.windows));
+    else run_pass<DQ, D, 1, NW, 64, LD, LD, RING_Q, false, MQ>(q, w, smem, nullptr, MQ(q, x, s.ring, s.windows));
+}
+
+template <int MODE, int D, int QB, int NW, int LD1, int LD2, int OCC, int RING, bool BIAS, bool DROP>
+int launch_pass(Params p, const Extra &x, hipStream_t stream) {
+    using C = Cfg<MODE, D, QB, NW, 64, LD1, LD2, RING>;
+    const long long wgs = tiles_of<C>(p);
+    p.in_order = batch_order(p, wgs, C::BM);
+    return enqueue(sigattn_mod<MODE, D, QB, NW, LD1, LD2, OCC, RING, BIAS, DROP>, wgs, C::THREADS, C::LDS_BYTES, stream, p, x);
+}
+
+template <bool BIAS, bool DROP>
+int launch_fwd(const Params &p, const Extra &x, int d, hipStream_t stream) {
+    if (d == 64) return launch_pass<FWD, 64, 1, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
+    return launch_pass<FWD, 128, 1, 8, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
+}
+
+template <bool BIAS, bool DROP>
+int launch_bwd(Params kv, Params q, const Extra &x, int d, hipStream_t stream) {
+    if (d == 64) {
+        using C = Cfg<DKDV, 64, 1, 4, 64, 72, 72, 8>;
+        static_assert(C::LDS_BYTES == Cfg<DQ, 64, 1, 4, 64, 72, 72, 4>::LDS_BYTES, "one LDS size for both passes");
+        const long long kv_tiles = tiles_of<C>(kv), q_tiles = tiles_of<C>(q);
+        kv.in_order = q.in_order = batch_order(kv, kv_tiles + q_tiles, C::BM) || batch_order(q, kv_tiles + q_tiles, C::BM);
+        const int q_first = kv.N_str < q.N_str;                // the pass whose workgroups stream more rows starts
+        return enqueue(sigattn_mod_bwd<64, 4, 72, 2, 8, 4, BIAS, DROP>, kv_tiles + q_tiles, C::THREADS, C::LDS_BYTES, stream, kv, q, x, q_first,
+                       (int)(q_first ? q_tiles : kv_tiles));
+    }
+    if (const int e = launch_pass<DKDV, 128, 1, 4, 144, 144, 1, 4, BIAS, DROP>(kv, x, stream)) return e;
+    return launch_pass<DQ, 128, 1, 8, 144, 136, 1, 4, BIAS, DROP>(q, x, stream);
+}
+
+// defined in sigattn_rel.hip, sigattn_dropout.hip, sigattn_rel_dropout.hip
+int fwd_rel(const Params &p, const Extra &x, int d, hipStream_t stream);
+int bwd_rel(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream);
+int fwd_dropout(const Params &p, const Extra &x, int d, hipStream_t stream);
+int bwd_dropout(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream);
+int fwd_rel_dropout(const Params &p, const Extra &x, int d, hipStream_t stream);
+int bwd_rel_dropout(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream);
+
+}  // namespace mod
+}  // namespace sigattn
