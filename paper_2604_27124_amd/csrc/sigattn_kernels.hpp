@@ -947,8 +947,18 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             });
             mod.next_block();
         }
-        if constexpr (Mod::SUMMED) mod.sum(dsbuf[PAR][0]);
-        if constexpr (Mod::SIFTED || Mod::SUMMED) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (Mod::SIFTED) __builtin_amdgcn_sched_barrier(0);
+    };
+    // SUMMED: both blocks of a tile, whose dS registers are intact until the step behind them.  `slot` is a ring slot that
+    // nobody reads before it is written again: the rows of it that this wave itself writes are the wave's scratch.
+    auto sums = [&](auto slot) {
+        if constexpr (Mod::SUMMED) {
+            static_assert(LD1 * 2 * (64 / C::CH) >= 1024 + 2 * (C::LM1 == 2 ? 8 : 0) && LD2 * 2 * (64 / C::CH) >= 1024 && C::LM2 == 0 && C::PER == 2, "scratch");
+            const int own = wave * (64 / C::CH), row = slot.get() * BN + own;
+            mod.sum(reinterpret_cast<unsigned char *>(y1s + row * LD1 + lds_shift<C::LM1>(own)), RPI * LD1 * 2,
+                    reinterpret_cast<unsigned char *>(y2s + row * LD2), RPI * LD2 * 2, dsbuf[0][0], dsbuf[1][0]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     auto tile_body = [&](auto slot_c) {            // from the second block of a tile through the first of the next
         constexpr int slot = decltype(slot_c)::value;
@@ -960,6 +970,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(READS_AFTER) : "memory");
         if constexpr (!LOAD_EARLY) load_tile();
         finish(IntC<1>{});
+        sums(IntC<(slot + 3) & (C::NBUF - 1)>{});      // the tile before this one; stored next: two steps on
         step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0);
     };
     // P and dS of the streamed rows behind the valid length, in block nb of the last tile: exact zeros, as packed for the
@@ -991,7 +1002,6 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     for (;;) {
         // the tiles stored last are visible, and nobody reads the slot that is written next
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if constexpr (Mod::SUMMED) mod.clear();
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
@@ -1054,6 +1064,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 mask_block(nb_);
                 finish(nb_);
             });
+            sums(DynInt{(slot_rt + 2) & (C::NBUF - 1)});   // no tile of its own: last read before the barrier behind the tile before
             const DynInt slot_next{(slot_rt + 1) & (C::NBUF - 1)};
             step(T_{}, F_{}, T_{}, IntC<0>{}, slot_next, NoStore{}, 0);
             if (more) {

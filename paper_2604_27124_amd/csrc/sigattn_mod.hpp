@@ -61,14 +61,12 @@ struct Mods {
     static constexpr bool BIASED = BIAS, SIFTED = DROP, SUMMED = SUM;
     static constexpr int BM = 32 * QB * NW, THREADS = 64 * NW;
     static constexpr int RING = 512, MIRROR = 32;              // floats; what is read past the end is kept there again
-    static constexpr int WINDOW = 160;                         // floats a wave: two halves of 64, 92 apart (disjoint banks)
     static_assert(BM + 160 <= RING, "live entries: an owner tile, the tile in hand and two more");
     static_assert(!SUM || (MODE == DQ && QB == 1), "sums ride on the dQ pass");
 
     const Params &p;
     const Extra &x;
     float *const ring;                                         // LDS [RING + MIRROR]
-    float *const windows;                                      // LDS [NW][WINDOW]
     int h, n, ns, m0, start_pos;
     int wave, lane;
 
@@ -86,10 +84,10 @@ struct Mods {
     float *out_row;
     int k, first, last, entries;
     bool active, open_window;
-    f32x4 far;
+    f32x4 acc;                                                 // near: four distances a lane; far: every row holds 16 sums
     float below;
 
-    __device__ __forceinline__ Mods(const Params &p_, const Extra &x_, float *ring_, float *windows_) : p(p_), x(x_), ring(ring_), windows(windows_) {}
+    __device__ __forceinline__ Mods(const Params &p_, const Extra &x_, float *ring_) : p(p_), x(x_), ring(ring_) {}
 
     // ---------------------------------------------------------------- bias
     // Distance (streamed - owner) `d` -> value; 0 for distances that no valid pair has, which padding alone reads.
@@ -136,7 +134,7 @@ struct Mods {
             active = 32 * ob < n;
             open_window = false;
             out_row = x.part + (((size_t)z * p.H + h) * blocks + ob) * (size_t)(entries + FAR);
-            far = f32x4{0.f, 0.f, 0.f, 0.f};
+            acc = f32x4{0.f, 0.f, 0.f, 0.f};
             below = 0.f;
         }
     }
@@ -262,60 +260,111 @@ struct Mods {
     }
 
     // ---------------------------------------------------------------- sums of dS
-    // Near blocks: each half of a wave adds its values into a window of its own over the 63 distances of the block, in LDS.
-    // The lanes of a half hold different distances in every instruction and a wave's LDS operations complete in order, so
-    // the order of every sum is fixed.  Then the 32 distances that no later block reaches go out and the window moves on.
-    // The summands are the bf16 values that also feed dQ.
-    __device__ __forceinline__ void clear() {
-        float *const w = windows + wave * WINDOW;
-        for (int e = lane; e < WINDOW; e += 64) w[e] = 0.f;
+    // A near block: the bf16 values that also feed dQ (two rows a register) go to LDS as 32 columns (queries) of 32 words, moved up
+    // by a word every second column, so that what belongs to one distance lies in one line: word u of an odd column holds
+    // distances 2 u and 2 u + 1 of the block's 63, of an even column 2 u + 1 and 2 u + 2; the rest of a column is zeros.  Columns c % 4 lie in four
+    // pieces of scratch, and the 16 lanes that read one add up eight columns, four distances a lane.  The four groups of
+    // lanes are joined when the 32 distances that no later block reaches go out; the others move down by as much.
+    // Every sum has its order: no atomics.  (With ds_add_f32 into such a window a block took 16 of them, at about a lane a
+    // clock: backward of B = 256, H = 12, N = 512 1657 us.)
+    static constexpr int ROW_SHR_1 = 0x111, ROW_SHL_8 = 0x108;
+    template <int CTRL>
+    __device__ __forceinline__ static float moved(const float v) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+    }
+    __device__ __forceinline__ static float join32(const float a, const float b) {     // lower half: a of both halves, upper: b
+        const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+        return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+    }
+    __device__ __forceinline__ static float join16(const float a, const float b) {     // the same for pairs of rows of 16
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+        return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
     }
     __device__ __forceinline__ void flush() {
-        const int c = lane & 31, g = lane >> 5;
-        float *const w = windows + wave * WINDOW + 92 * g;
-        const float done = w[c], rest = w[c + 32];
-        w[c] = rest;
-        w[c + 32] = 0.f;
-        const float other = __shfl_xor(done, 32, 64);
-        if (g == 0) out_row[32 * (k - first) + c] = done + other;
+        const float out = join16(join32(acc[0], acc[2]), join32(acc[1], acc[3]));
+        const int v = lane & 15;
+        if (v < 8) out_row[32 * (k - first) + 4 * v + (lane >> 4)] = out;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = moved<ROW_SHL_8>(acc[i]);
     }
-    __device__ __forceinline__ void sum(const u32x4 (&packed)[2]) {
-        if (!active) return;                                   // uniform
-        const int c = lane & 31, g = lane >> 5;
-        u32x4 ds[2] = {packed[0], packed[1]};
-        if (n - m0 - 32 * wave < 32) {                         // rows behind the valid queries: a key of Inf would make them NaN
-            const unsigned ok = m0 + 32 * wave + c < n ? ~0u : 0u;
+    __device__ __forceinline__ void sum_block(unsigned char *const put, const unsigned char *const get, const u32x4 (&ds)[2]) {
+        if (k >= first && k <= last) {                         // uniform
+            if (!open_window) { below = acc[0]; acc = f32x4{0.f, 0.f, 0.f, 0.f}; open_window = true; }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ds[i / 4][i % 4] &= ok;
-        }
-        if (k >= first && k <= last) {
-            if (!open_window) { below = far[0]; far = f32x4{0.f, 0.f, 0.f, 0.f}; open_window = true; }
-            float *const w = windows + wave * WINDOW + 92 * g + 31 - c + 4 * g;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const unsigned v = ds[i / 4][i % 4];
-                const int r = 8 * (i / 2) + 2 * (i % 2);
-                __hip_atomic_fetch_add(w + r, __builtin_bit_cast(float, v << 16), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-                __hip_atomic_fetch_add(w + r + 1, __builtin_bit_cast(float, v & 0xFFFF0000u), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+            for (int q = 0; q < 4; ++q) {                      // rows 8 q + 4 g + 0..3
+                unsigned *const w = reinterpret_cast<unsigned *>(put) + 4 * q;
+                w[0] = ds[q / 2][2 * (q % 2)];
+                w[1] = ds[q / 2][2 * (q % 2) + 1];
             }
+            asm volatile("" ::: "memory");
+            float t[4] = {0.f, 0.f, 0.f, 0.f};
+            // (1, 0) and (0, 1) in scalar registers: as inline constants their packed form would be the instruction's own affair
+            unsigned lo = 0x00003F80u, hi = 0x3F800000u;
+            asm("" : "+s"(lo), "+s"(hi));
+            const bf16x2 one_lo = __builtin_bit_cast(bf16x2, lo), one_hi = __builtin_bit_cast(bf16x2, hi);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const u32x2 w = *reinterpret_cast<const u32x2 *>(get + 128 * j);
+                const unsigned w0 = w[0], w1 = w[1];           // a bit cast of a vector's element itself reads element 0
+                const bf16x2 a = __builtin_bit_cast(bf16x2, w0), b = __builtin_bit_cast(bf16x2, w1);
+                t[0] = __builtin_amdgcn_fdot2_f32_bf16(a, one_lo, t[0], false);
+                t[1] = __builtin_amdgcn_fdot2_f32_bf16(a, one_hi, t[1], false);
+                t[2] = __builtin_amdgcn_fdot2_f32_bf16(b, one_lo, t[2], false);
+                t[3] = __builtin_amdgcn_fdot2_f32_bf16(b, one_hi, t[3], false);
+            }
+            asm volatile("" ::: "memory");
+            const bool even = ((lane >> 4) & 1) == 0;          // lanes of even columns are a distance ahead
+            const float t3 = moved<ROW_SHR_1>(t[3]);
+            acc[0] += even ? t3 : t[0];
+            acc[1] += even ? t[0] : t[1];
+            acc[2] += even ? t[1] : t[2];
+            acc[3] += even ? t[2] : t[3];
             flush();
         } else {
-            if (k > last && open_window) { flush(); open_window = false; }
+            if (k > last && open_window) { flush(); acc = f32x4{0.f, 0.f, 0.f, 0.f}; open_window = false; }
             bf16x8 ones;
 #pragma unroll
             for (int i = 0; i < 8; ++i) ones[i] = (bf16_t)1.0f;
-            far = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[0]), far, 0, 0, 0);
-            far = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[1]), far, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[0]), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[1]), acc, 0, 0, 0);
         }
         ++k;
     }
-    // Behind the last block: what is left in the window, and the far sums.
+    // A tile's two blocks.  Scratch of this wave: 1024 bytes each at a, a + a_step, b, b + b_step.
+    __device__ __forceinline__ void sum(unsigned char *const a, const int a_step, unsigned char *const b, const int b_step, const u32x4 (&first_ds)[2],
+                                        const u32x4 (&second_ds)[2]) {
+        if (!active) return;                                   // uniform
+        const int c = lane & 31, g = lane >> 5;
+        u32x4 d0[2] = {first_ds[0], first_ds[1]}, d1[2] = {second_ds[0], second_ds[1]};
+        if (n - m0 - 32 * wave < 32) {                         // rows behind the valid queries: a key of Inf would make them NaN
+            const unsigned ok = m0 + 32 * wave + c < n ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d0[i / 4][i % 4] &= ok;
+                d1[i / 4][i % 4] &= ok;
+            }
+        }
+        asm volatile("" ::: "memory");
+        if (k <= last && k + 1 >= first) {
+            const u32x4 z4 = {0u, 0u, 0u, 0u};
+            *reinterpret_cast<u32x4 *>(a + 16 * lane) = z4;
+            *reinterpret_cast<u32x4 *>(a + a_step + 16 * lane) = z4;
+            *reinterpret_cast<u32x4 *>(b + 16 * lane) = z4;
+            *reinterpret_cast<u32x4 *>(b + b_step + 16 * lane) = z4;
+        }
+        asm volatile("" ::: "memory");
+        auto piece = [&](const int i) { return (i & 2 ? b : a) + (i & 1 ? (i & 2 ? b_step : a_step) : 0); };
+        unsigned char *const put = piece(c & 3) + (c >> 2) * 128 + 4 * (15 - (c >> 1)) + 8 * g;
+        const unsigned char *const get = piece(lane >> 4) + 8 * (lane & 15);
+        sum_block(put, get, d0);
+        sum_block(put, get, d1);
+    }
+    // Behind the last block: what is left in the window, and the far sums (row 0 of the accumulators, lanes 0 to 15).
     __device__ __forceinline__ void close() {
         if (!active) return;
-        if (open_window) flush();
+        if (open_window) { flush(); acc = f32x4{0.f, 0.f, 0.f, 0.f}; }
         const bool all_below = k <= first;                     // not one block was near, or beyond
-        float v = lane < 16 ? far[0] : 0.f;
-        float u = lane < 16 ? below : 0.f;
+        float v = lane < 16 ? acc[0] : 0.f, u = lane < 16 ? below : 0.f;
 #pragma unroll
         for (int off = 8; off >= 1; off >>= 1) {
             v += __shfl_xor(v, off, 64);

@@ -22,29 +22,39 @@ __device__ __forceinline__ int clamped(int v, int lo, int hi) { return v < lo ? 
 
 __device__ __forceinline__ int start_of(const Lengths &l, int z) { return l.start ? clamped(l.start[z], -(1 << 29), 1 << 29) : 0; }
 
-// Group s of `groups` adds up the rows of sequences s, s + groups, ...: [group][H][entries + FAR].  A workgroup takes 32 entries of a
-// head; its eight groups of 32 lanes take the rows of a sequence in turn.  Fixed order, no atomics.
-__global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const Extra x, const int groups) {
+// Sums over rows, in fixed order and without atomics.  Group s of `groups` takes sequences s, s + groups, ...: [group][H][entries + FAR].  A
+// workgroup takes 32 entries of a head; of its eight groups of 32 lanes `seqs` take a sequence each, and the others share the
+// rows of these.
+__global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const Extra x, const int groups, const int seqs) {
     __shared__ float s[8][32];
     const int entries = RowSums::entries(x.reach, l.L_q, l.L_k), chunks = entries / 32 + 1;
     const int chunk = blockIdx.x % chunks, rest = blockIdx.x / chunks, h = rest % l.H, group = rest / l.H;
-    const int c = threadIdx.x & 31, mine = threadIdx.x >> 5;
+    const int c = threadIdx.x & 31, mine = threadIdx.x >> 5, step = 8 / seqs;
     const int blocks = (l.L_q + 31) / 32;
     const bool far = chunk == chunks - 1;
+    const size_t stride = (size_t)(entries + mod::FAR);
     float total = 0.f;
-    for (int z = group; z < l.B; z += groups) {
+    for (long long z = group + (long long)groups * (mine % seqs); z < l.B; z += (long long)groups * seqs) {
         const int nq = clamped(l.q[z], 0, l.L_q), ns = clamped(l.k[z], 0, l.L_k);
         if (nq == 0 || ns == 0) continue;
         const RowSums r(x.reach, start_of(l, z), blocks);
         const int k = r.first + chunk, key_blocks = 2 * ((ns + 63) / 64);
-        const float *const rows = x.part + ((size_t)z * l.H + h) * blocks * (size_t)(entries + mod::FAR) + 32 * chunk + c;
+        // rows that have the entry: b = k + ob is a near block's, or b - 1 is (what the last near block leaves behind)
+        int from = -k, to = key_blocks - k;                                    // key blocks 0 .. key_blocks - 1
+        if (chunk > 0) ++to;                                                   // and the one behind, of diagonal k - 1
+        if (k > r.last) { ++from; if (k > r.last + 1 || chunk == 0) to = from; }   // only as what is left
+        const int all = (nq + 31) / 32;
+        if (far) { from = 0; to = c < 2 ? all : 0; }
+        from = from < 0 ? 0 : from;
+        to = to > all ? all : to;
+        const float *const rows = x.part + ((size_t)z * l.H + h) * blocks * stride + 32 * chunk + c;
         float t = 0.f;
-        for (int ob = mine; 32 * ob < nq; ob += 8) {
-            // written: what a near block sent out, and what the last near block left behind
-            const bool here = k <= r.last && k + ob >= 0 && k + ob < key_blocks;
-            const bool left = chunk > 0 && k - 1 <= r.last && k - 1 + ob >= 0 && k - 1 + ob < key_blocks;
-            if (far ? c < 2 : here || left) t += rows[ob * (size_t)(entries + mod::FAR)];
+        int ob = from + mine / seqs;
+        for (; ob + 3 * step < to; ob += 4 * step) {                           // four loads in flight
+            const float a = rows[ob * stride], b = rows[(ob + step) * stride], e = rows[(ob + 2 * step) * stride], f = rows[(ob + 3 * step) * stride];
+            t += (a + b) + (e + f);
         }
+        for (; ob < to; ob += step) t += rows[ob * stride];
         const float cb = __builtin_amdgcn_exp2f(__builtin_fminf(__builtin_fmaxf(-l.bias[z] * 1.4426950408889634f, -126.0f), 126.0f));
         total += t * (cb * x.inv_keep);
     }
@@ -54,29 +64,52 @@ __global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const E
         float t = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) t += s[i][c];
-        x.by_distance[((size_t)group * l.H + h) * (entries + mod::FAR) + 32 * chunk + c] = t;
+        x.by_distance[((size_t)group * l.H + h) * stride + 32 * chunk + c] = t;
     }
 }
 
-// dtable[b][h]: a wave for a bucket, over the distances of every group.
+// dtable[b][h] for 16 buckets of a head: the entries of all groups (of one group where every sequence has a start of its own), a
+// thousand at a time, with their buckets, in LDS; each wave goes through them for its four buckets.
+constexpr int TABLE_BUCKETS = 16, TABLE_ENTRIES = 1024;
 __global__ void __launch_bounds__(256) sigattn_rel_table(const Lengths l, const Extra x, const int groups, bf16_t *dtable) {
-    const int wide = (x.num_buckets + 3) / 4;
-    const int h = blockIdx.x / wide, b = blockIdx.x % wide * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (b >= x.num_buckets) return;
+    __shared__ float value[TABLE_ENTRIES];
+    __shared__ int bucket[TABLE_ENTRIES];
+    const int wide = (x.num_buckets + TABLE_BUCKETS - 1) / TABLE_BUCKETS;
+    const int h = blockIdx.x / wide, b0 = blockIdx.x % wide * TABLE_BUCKETS + 4 * (threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int entries = RowSums::entries(x.reach, l.L_q, l.L_k);
-    auto bucket = [&](int t) { return clamped(x.buckets[clamped(t, -x.reach, x.reach) + x.reach], 0, x.num_buckets - 1); };
-    float total = 0.f;
-    for (int g = 0; g < groups; ++g) {
-        const int start = start_of(l, g);                      // groups share a start only if there is none
+    const size_t stride = (size_t)(entries + mod::FAR), head = stride * l.H;
+    float total[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < groups; g = l.start ? g + 1 : groups) {
+        const int start = start_of(l, g), count = l.start ? 1 : groups;        // without starts all sequences have the same distances
         const RowSums r(x.reach, start, (l.L_q + 31) / 32);
-        const float *const d = x.by_distance + ((size_t)g * l.H + h) * (entries + mod::FAR);
-        for (int e = lane; e < entries; e += 64)
-            if (bucket(32 * r.first - start - 31 + e) == b) total += d[e];
-        if (lane < 2 && bucket(lane == 0 ? -x.reach : x.reach) == b) total += d[entries + lane];
+        const float *const from = x.by_distance + g * head + h * stride;
+        for (int e0 = 0; e0 < entries + 2; e0 += TABLE_ENTRIES) {
+            __syncthreads();
+            const int most = entries + 2 - e0 < TABLE_ENTRIES ? entries + 2 - e0 : TABLE_ENTRIES;
+            for (int i = threadIdx.x; i < most; i += 256) {
+                const int e = e0 + i, t = e < entries ? 32 * r.first - start - 31 + e : (e == entries ? -x.reach : x.reach);
+                bucket[i] = clamped(x.buckets[clamped(t, -x.reach, x.reach) + x.reach], 0, x.num_buckets - 1);
+                float v = 0.f;
+                int c = 0;
+                for (; c + 4 <= count; c += 4) v += (from[c * head + e] + from[(c + 1) * head + e]) + (from[(c + 2) * head + e] + from[(c + 3) * head + e]);
+                for (; c < count; ++c) v += from[c * head + e];
+                value[i] = v;
+            }
+            __syncthreads();
+            for (int i = lane; i < most; i += 64) {
+                const int b = bucket[i];
+                const float v = value[i];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) total[w] += b == b0 + w ? v : 0.f;
+            }
+        }
     }
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off, 64);
-    if (lane == 0) dtable[(size_t)b * l.H + h] = (bf16_t)total;
+    for (int w = 0; w < 4; ++w) {
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) total[w] += __shfl_xor(total[w], off, 64);
+        if (lane == 0 && b0 + w < x.num_buckets) dtable[(size_t)(b0 + w) * l.H + h] = (bf16_t)total[w];
+    }
 }
 
 bool aligned(const void *p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -192,13 +225,15 @@ int backward(const void *q, const void *k, const void *v, const void *d_o, void 
     if (!rel) return mod::bwd_dropout(pk, pq, x, d, s);
 
     const int entries = RowSums::entries(rel->reach, L_q, L_k), groups = rel->q_start || B < 16 ? B : 16;
-    const long long row_wgs = (long long)groups * H * (entries / 32 + 1), table_wgs = (long long)H * ((rel->num_buckets + 3) / 4);
+    const long long row_wgs = (long long)groups * H * (entries / 32 + 1), table_wgs = (long long)H * ((rel->num_buckets + TABLE_BUCKETS - 1) / TABLE_BUCKETS);
+    int seqs = 1;
+    while (seqs < 8 && seqs * 2LL * groups <= B) seqs *= 2;
     if (row_wgs > 2147483647LL || table_wgs > 2147483647LL) return SIGATTN_ERR_TOO_LARGE;
     x.part = static_cast<float *>(workspace);
     x.by_distance = x.part + row_floats(B, L_q, L_k, H, rel->reach);
     if (int e = drop ? mod::bwd_rel_dropout(pk, pq, x, d, s) : mod::bwd_rel(pk, pq, x, d, s)) return e;
     const Lengths l{seqlens_q, seqlens_k, rel->q_start, bias, L_q, L_k, H, B};
-    if (int e = enqueue(sigattn_rel_rows, row_wgs, 256, 0, s, l, x, groups)) return e;
+    if (int e = enqueue(sigattn_rel_rows, row_wgs, 256, 0, s, l, x, groups, seqs)) return e;
     return enqueue(sigattn_rel_table, table_wgs, 256, 0, s, l, x, groups, static_cast<bf16_t *>(dtable));
 }
 

@@ -6,29 +6,25 @@
 namespace sigattn {
 namespace mod {
 
-template <int NW>
 struct Scratch {
-    union {                                                    // the windows are cleared behind the first barrier after the mapping
-        MapScratch map;
-        float windows[NW * 160];
-    };
+    MapScratch map;
     float ring[512 + 32];
 };
 
 template <int MODE, int D, int QB, int NW, int LD1, int LD2, int OCC, int RING, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod(const Params p, const Extra x) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ Scratch<NW> s;
+    __shared__ Scratch s;
     using C = Cfg<MODE, D, QB, NW, 64, LD1, LD2, RING>;
     using M = Mods<MODE, QB, NW, BIAS, DROP, BIAS && MODE == DQ>;
-    run_pass<MODE, D, QB, NW, 64, LD1, LD2, RING, false, M>(p, map_work<C::BM, C::THREADS>(p, blockIdx.x, s.map), smem, nullptr, M(p, x, s.ring, s.windows));
+    run_pass<MODE, D, QB, NW, 64, LD1, LD2, RING, false, M>(p, map_work<C::BM, C::THREADS>(p, blockIdx.x, s.map), smem, nullptr, M(p, x, s.ring));
 }
 
 // d = 64: both passes of the backward in one launch, as in sigattn_bwd_kernel.
 template <int D, int NW, int LD, int OCC, int RING_KV, int RING_Q, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod_bwd(const Params kv, const Params q, const Extra x, const int q_first, const int first_tiles) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ Scratch<NW> s;
+    __shared__ Scratch s;
     using C = Cfg<DKDV, D, 1, NW, 64, LD, LD, RING_KV>;
     using MK = Mods<DKDV, 1, NW, BIAS, DROP, false>;
     using MQ = Mods<DQ, 1, NW, BIAS, DROP, BIAS>;
@@ -49,8 +45,8 @@ __global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod_bwd(const Params kv,
         const int rest = id < first_tiles ? id : id - first_tiles;
         w = is_kv ? map_work<C::BM, C::THREADS>(kv, rest, s.map) : map_work<C::BM, C::THREADS>(q, rest, s.map);
     }
-    if (is_kv) run_pass<DKDV, D, 1, NW, 64, LD, LD, RING_KV, false, MK>(kv, w, smem, nullptr, MK(kv, x, s.ring, s.windows));
-    else run_pass<DQ, D, 1, NW, 64, LD, LD, RING_Q, false, MQ>(q, w, smem, nullptr, MQ(q, x, s.ring, s.windows));
+    if (is_kv) run_pass<DKDV, D, 1, NW, 64, LD, LD, RING_KV, false, MK>(kv, w, smem, nullptr, MK(kv, x, s.ring));
+    else run_pass<DQ, D, 1, NW, 64, LD, LD, RING_Q, false, MQ>(q, w, smem, nullptr, MQ(q, x, s.ring));
 }
 
 template <int MODE, int D, int QB, int NW, int LD1, int LD2, int OCC, int RING, bool BIAS, bool DROP>
@@ -63,7 +59,10 @@ int launch_pass(Params p, const Extra &x, hipStream_t stream) {
 
 template <bool BIAS, bool DROP>
 int launch_fwd(const Params &p, const Extra &x, int d, hipStream_t stream) {
-    if (d == 64) return launch_pass<FWD, 64, 1, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
+    if (d == 64) {
+        if (p.N <= 128 || (long long)p.B * p.H * ((p.N + 255) / 256) <= 256) return launch_pass<FWD, 64, 1, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
+        return launch_pass<FWD, 64, 2, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
+    }
     return launch_pass<FWD, 128, 1, 8, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
 }
 
