@@ -77,7 +77,7 @@ struct Mods {
     float value;
 
     // dropout
-    unsigned key0, key1, c3, c2, row, group;                   // row, group: counter words of owner block 0, this block
+    unsigned keep, key0, key1, c3, c2, row, group;             // row, group: counter words of owner block 0, this block
     unsigned ph[DROP ? QB : 1][4], stays[DROP ? QB : 1];
 
     // sums
@@ -117,6 +117,7 @@ struct Mods {
             bucket = bucket_at(next_x + lane);
         }
         if constexpr (DROP) {
+            keep = __builtin_amdgcn_readfirstlane(x.keep);
             const u64 seed = x.rng[0], offset = x.rng[1];
             key0 = __builtin_amdgcn_readfirstlane((unsigned)seed);
             key1 = __builtin_amdgcn_readfirstlane((unsigned)(seed >> 32));
@@ -173,7 +174,12 @@ struct Mods {
     // ---------------------------------------------------------------- dropout
     __device__ __forceinline__ float scale() const { return x.inv_keep; }
 
-    __device__ __forceinline__ static unsigned majority(unsigned a, unsigned b, unsigned c) { return (a & b) | (c & (a | b)); }
+    // Functions of three words in one instruction each; the byte is the function's truth table.
+    __device__ __forceinline__ static unsigned majority(unsigned a, unsigned b, unsigned c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0xE8); }
+    __device__ __forceinline__ static unsigned xor3(unsigned a, unsigned b, unsigned c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+    __device__ __forceinline__ static unsigned choose(unsigned mask, unsigned a, unsigned b) { return __builtin_amdgcn_bitop3_b32(mask, a, b, 0xCA); }
+    // All ones where bit `at` of v is set, else zero.
+    __device__ __forceinline__ static unsigned smear(unsigned v, int at) { return (unsigned)__builtin_amdgcn_sbfe((int)v, at, 1); }
 
     // Part `item` of the generator of owner block qb: seven rounds of Philox4x32 (Salmon, Moraes, Dror, Shaw 2011), then the 16
     // decisions of a lane.  Decision t takes bits t and t + 8 of each of the four words as its byte; its 16-bit number u is that
@@ -191,20 +197,18 @@ struct Mods {
         if constexpr (item < 7) {
             const u64 a = (u64)0xD2511F53u * c[0], b = (u64)0xCD9E8D57u * c[2];
             const unsigned k0 = key0 + item * 0x9E3779B9u, k1 = key1 + item * 0xBB67AE85u;
-            const unsigned n0 = (unsigned)(b >> 32) ^ c[1] ^ k0, n2 = (unsigned)(a >> 32) ^ c[3] ^ k1;
+            const unsigned n0 = xor3((unsigned)(b >> 32), c[1], k0), n2 = xor3((unsigned)(a >> 32), c[3], k1);
             c[0] = n0; c[1] = (unsigned)b; c[2] = n2; c[3] = (unsigned)a;
         } else {
             unsigned m = 0;
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
-                const unsigned bit = 0u - ((x.keep >> s) & 1u);
-                m = majority(c[(7 - s) / 2] >> (8 * ((7 - s) % 2)), m, bit);
+                m = majority(c[(7 - s) / 2] >> (8 * ((7 - s) % 2)), m, smear(keep, s));
             }
             m = __builtin_amdgcn_alignbit(m, m, 16);
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
-                const unsigned bit = 0u - ((x.keep >> (8 + s)) & 1u);
-                m = majority(c[s / 2] >> (8 * (s % 2)), m, bit);
+                m = majority(c[s / 2] >> (8 * (s % 2)), m, smear(keep, 8 + s));
             }
             stays[qb] = MODE == DKDV ? turned(m) : m;
         }
@@ -213,12 +217,15 @@ struct Mods {
     // keys and queries exchanged in the result.  The words of both halves of the wave are joined into rows of 32 bits, and
     // each of five steps exchanges one bit of the lane's number with the bit of the position that stands for the same bit of
     // the other tensor's row.
+    // One such step: `other` is the word of the lane whose number differs in one bit (`upper` smeared: it is set in this one's),
+    // STRIDE the bit of the position.  Both shifts of it side by side, then the lane's own part and the other's.
     template <int STRIDE>
-    __device__ __forceinline__ static unsigned exchange(const unsigned own, const unsigned other, const bool upper) {
+    __device__ __forceinline__ static unsigned exchange(const unsigned own, const unsigned other, const unsigned upper) {
         constexpr unsigned LOW = STRIDE == 1 ? 0x55555555u : STRIDE == 2 ? 0x33333333u : STRIDE == 4 ? 0x0F0F0F0Fu : STRIDE == 8 ? 0x00FF00FFu : 0x0000FFFFu;
-        const unsigned moved = __builtin_amdgcn_alignbit(other, other, upper ? STRIDE : 32 - STRIDE);
-        const unsigned mine = upper ? ~LOW : LOW;
-        return (own & mine) | (moved & ~mine);
+        const unsigned crossed = STRIDE == 16  ? __builtin_amdgcn_alignbit(other, other, 16)
+                                 : STRIDE == 8 ? __builtin_amdgcn_perm(other, other, 0x02030001)
+                                               : choose(LOW, other >> STRIDE, other << STRIDE);
+        return choose(LOW ^ upper, own, crossed);
     }
     template <int CTRL>
     __device__ __forceinline__ static unsigned dpp(const unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
@@ -227,12 +234,12 @@ struct Mods {
         m = (m & 0x00FF00FFu) << (8 * g);
         const auto halves = __builtin_amdgcn_permlane32_swap(m, m, false, false);     // {lower half's words, upper half's} in every lane
         unsigned v = halves[0] | halves[1];
-        v = exchange<16>(v, dpp<0xB1>(v), lane & 1);                                   // quad_perm 1, 0, 3, 2
-        v = exchange<1>(v, dpp<0x4E>(v), lane & 2);                                    // quad_perm 2, 3, 0, 1
-        v = exchange<8>(v, dpp<0x1B>(dpp<0x141>(v)), lane & 4);                        // half mirror, then quad_perm 3, 2, 1, 0
-        v = exchange<2>(v, dpp<0x128>(v), lane & 8);                                   // rotation of a row of 16 by 8
+        v = exchange<16>(v, dpp<0xB1>(v), smear(lane, 0));                                   // quad_perm 1, 0, 3, 2
+        v = exchange<1>(v, dpp<0x4E>(v), smear(lane, 1));                                    // quad_perm 2, 3, 0, 1
+        v = exchange<8>(v, dpp<0x1B>(dpp<0x141>(v)), smear(lane, 2));                        // half mirror, then quad_perm 3, 2, 1, 0
+        v = exchange<2>(v, dpp<0x128>(v), smear(lane, 3));                                   // rotation of a row of 16 by 8
         const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        v = exchange<4>(v, lane & 16 ? rows[0] : rows[1], lane & 16);
+        v = exchange<4>(v, choose(smear(lane, 4), rows[0], rows[1]), smear(lane, 4));
         return v >> (8 * g);
     }
 

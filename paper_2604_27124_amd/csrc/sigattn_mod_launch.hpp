@@ -69,12 +69,12 @@ int launch_fwd(const Params &p, const Extra &x, int d, hipStream_t stream) {
 template <bool BIAS, bool DROP>
 int launch_bwd(Params kv, Params q, const Extra &x, int d, hipStream_t stream) {
     if (d == 64) {
-        using C = Cfg<DKDV, 64, 1, 4, 64, 72, 72, 8>;
+        using C = Cfg<DKDV, 64, 1, 4, 64, 72, 72, 4>;
         static_assert(C::LDS_BYTES == Cfg<DQ, 64, 1, 4, 64, 72, 72, 4>::LDS_BYTES, "one LDS size for both passes");
         const long long kv_tiles = tiles_of<C>(kv), q_tiles = tiles_of<C>(q);
         kv.in_order = q.in_order = batch_order(kv, kv_tiles + q_tiles, C::BM) || batch_order(q, kv_tiles + q_tiles, C::BM);
         const int q_first = kv.N_str < q.N_str;                // the pass whose workgroups stream more rows starts
-        return enqueue(sigattn_mod_bwd<64, 4, 72, 2, 8, 4, BIAS, DROP>, kv_tiles + q_tiles, C::THREADS, C::LDS_BYTES, stream, kv, q, x, q_first,
+        return enqueue(sigattn_mod_bwd<64, 4, 72, 2, 4, 4, BIAS, DROP>, kv_tiles + q_tiles, C::THREADS, C::LDS_BYTES, stream, kv, q, x, q_first,
                        (int)(q_first ? q_tiles : kv_tiles));
     }
     if (const int e = launch_pass<DKDV, 128, 1, 4, 144, 144, 1, 4, BIAS, DROP>(kv, x, stream)) return e;
