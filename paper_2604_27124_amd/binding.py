@@ -28,7 +28,7 @@ EXPORTS = ("sigmoid_attn_version", "sigmoid_attn_strerror", "sigmoid_attn_fwd", 
            "sigmoid_attn_bwd_dq_dbias", "sigmoid_attn_bwd_dq_dbias_workspace_bytes",
            "sigmoid_attn_cross_bwd_dq_dbias", "sigmoid_attn_cross_bwd_dq_dbias_workspace_bytes",
            "sigmoid_attn_bwd_dq_dbias_static",
-           "sigmoid_attn_rel_fwd", "sigmoid_attn_rel_bwd", "sigmoid_attn_rel_bwd_workspace_bytes", "sigmoid_attn_rel_buckets",
+           "sigmoid_attn_rel_fwd", "sigmoid_attn_rel_bwd", "sigmoid_attn_rel_fwd_workspace_bytes", "sigmoid_attn_rel_bwd_workspace_bytes", "sigmoid_attn_rel_buckets",
            "sigmoid_attn_dropout_fwd", "sigmoid_attn_dropout_bwd", "sigmoid_attn_rel_dropout_fwd", "sigmoid_attn_rel_dropout_bwd")
 
 _lib = None
@@ -119,7 +119,9 @@ def load() -> ctypes.CDLL:
         lib.sigmoid_attn_rel_buckets.argtypes = [vp, ci, ci]
         lib.sigmoid_attn_rel_bwd_workspace_bytes.argtypes = sizes + [ci]
         lib.sigmoid_attn_rel_bwd_workspace_bytes.restype = sz
-        lib.sigmoid_attn_rel_fwd.argtypes = [vp] * 7 + [cf] + rel + sizes + [vp]
+        lib.sigmoid_attn_rel_fwd_workspace_bytes.argtypes = sizes
+        lib.sigmoid_attn_rel_fwd_workspace_bytes.restype = sz
+        lib.sigmoid_attn_rel_fwd.argtypes = [vp] * 7 + [cf] + rel + sizes + [vp, sz, vp]
         lib.sigmoid_attn_rel_bwd.argtypes = [vp] * 11 + [cf] + rel + sizes + [vp, sz, vp]
         lib.sigmoid_attn_dropout_fwd.argtypes = [vp] * 7 + [cf] + drop + sizes + [vp]
         lib.sigmoid_attn_dropout_bwd.argtypes = [vp] * 10 + [cf] + drop + sizes + [vp]
@@ -429,6 +431,10 @@ def sigmoid_attn_rel_buckets(num_buckets: int, reach: int):
     return out
 
 
+def sigmoid_attn_rel_fwd_workspace_bytes(B: int, L_q: int, L_k: int, H: int, d: int) -> int:
+    return int(load().sigmoid_attn_rel_fwd_workspace_bytes(B, L_q, L_k, H, d))
+
+
 def sigmoid_attn_rel_bwd_workspace_bytes(B: int, L_q: int, L_k: int, H: int, d: int, reach: int) -> int:
     return int(load().sigmoid_attn_rel_bwd_workspace_bytes(B, L_q, L_k, H, d, reach))
 
@@ -460,7 +466,7 @@ def _check_drop(q, p, rng):
     return float(p), rng.data_ptr()
 
 
-def _mod_fwd(name, q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, out, stream):
+def _mod_fwd(name, q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, out, workspace, stream):
     _check_cross(q, k, v)
     B, Lq, H, d = q.shape
     Lk = k.shape[1]
@@ -471,8 +477,14 @@ def _mod_fwd(name, q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, out, s
     more = (_check_rel(q, *rel) if rel else ()) + (_check_drop(q, *drop) if drop else ())
     with torch.cuda.device(q.device):
         out = _output(out, "out", q)
+        scratch = ()
+        if rel and not drop:                       # optional: without it the call is not split
+            if workspace is None and Lq <= 8:
+                need = sigmoid_attn_rel_fwd_workspace_bytes(B, Lq, Lk, H, d)
+                workspace = _scratch(need, q, stream) if need > 0 else None
+            scratch = _workspace_args(workspace, q)
         rc = getattr(load(), name)(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), seqlens_q.data_ptr(), seqlens_k.data_ptr(),
-                                   bias.data_ptr(), float(scale), *more, B, Lq, Lk, H, d, _stream_ptr(stream))
+                                   bias.data_ptr(), float(scale), *more, B, Lq, Lk, H, d, *scratch, _stream_ptr(stream))
     if rc != SIGATTN_OK:
         raise SigAttnError(rc)
     return out
@@ -511,10 +523,12 @@ def _mod_bwd(name, q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, rel, drop, d
     return grads
 
 
-def sigmoid_attn_rel_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, out=None, stream=None):
+def sigmoid_attn_rel_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, out=None, workspace=None,
+                         stream=None):
     """Forward pass with table[buckets[clamp(j - i - q_start, -reach, reach) + reach]][h] added to the scores.
-    table: bf16 [num_buckets, H]; buckets: int32 [2 * reach + 1] (sigmoid_attn_rel_buckets makes one); q_start: int32 [B] or None."""
-    return _mod_fwd("sigmoid_attn_rel_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), None, out, stream)
+    table: bf16 [num_buckets, H]; buckets: int32 [2 * reach + 1] (sigmoid_attn_rel_buckets makes one); q_start: int32 [B] or None.
+    The workspace (for up to eight queries against a long context) is allocated if None; an empty tensor stands for none."""
+    return _mod_fwd("sigmoid_attn_rel_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), None, out, workspace, stream)
 
 
 def sigmoid_attn_rel_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, dq=None, dk=None, dv=None,
@@ -526,7 +540,7 @@ def sigmoid_attn_rel_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float,
 
 def sigmoid_attn_dropout_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, p: float, rng, out=None, stream=None):
     """Forward pass with dropout of the attention weights.  rng: int64 [2] in device memory, seed and offset."""
-    return _mod_fwd("sigmoid_attn_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, None, (p, rng), out, stream)
+    return _mod_fwd("sigmoid_attn_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, None, (p, rng), out, None, stream)
 
 
 def sigmoid_attn_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, p: float, rng, dq=None, dk=None, dv=None, stream=None) -> Tuple:
@@ -537,7 +551,7 @@ def sigmoid_attn_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: fl
 def sigmoid_attn_rel_dropout_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, table, buckets, p: float, rng, q_start=None, out=None,
                                  stream=None):
     """Forward pass with the relative position bias and dropout."""
-    return _mod_fwd("sigmoid_attn_rel_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), (p, rng), out, stream)
+    return _mod_fwd("sigmoid_attn_rel_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), (p, rng), out, None, stream)
 
 
 def sigmoid_attn_rel_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, p: float, rng, q_start=None, dq=None,

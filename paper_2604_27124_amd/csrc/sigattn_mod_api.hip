@@ -1,6 +1,7 @@
 // Host side of the calls with a relative position bias and with dropout (include/sigmoid_attn.h), and the kernels that add up the
 // gradient of the bias table.
 #include "sigattn_mod_launch.hpp"
+#include "sigattn_rel_few.hpp"
 
 #include <cmath>
 
@@ -164,8 +165,22 @@ Extra extra(const Bias *rel, const Drop *drop) {
     return x;
 }
 
+// Few queries (sigattn_rel_few.hpp): parts of a (z, h)'s keys.  A part is at least 1024 keys long (its start, and the second launch, take as
+// long as reading some hundreds), and there are no more than give every CU two workgroups.
+int few_splits(int B, int L_k, int H) {
+    const long long room = 512 / ((long long)B * H), longest = ((long long)L_k + 1023) / 1024;
+    const long long s = room < longest ? room : longest;
+    return s < 1 ? 1 : (int)s;
+}
+int few_rows(int L_q) { return L_q == 1 ? 1 : L_q == 2 ? 2 : L_q <= 4 ? 4 : 8; }
+size_t few_bytes(int B, int L_q, int L_k, int H, int d) {
+    if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK || L_q > few::MOST) return 0;
+    const int s = few_splits(B, L_k, H);
+    return s == 1 ? 0 : (size_t)s * B * H * few_rows(L_q) * d * sizeof(float);
+}
+
 int forward(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
-            const Bias *rel, const Drop *drop, int B, int L_q, int L_k, int H, int d, void *stream) {
+            const Bias *rel, const Drop *drop, int B, int L_q, int L_k, int H, int d, void *workspace, size_t workspace_bytes, void *stream) {
     if (!o) return SIGATTN_ERR_INVALID_ARG;
     if (int e = check(q, k, v, seqlens_q, seqlens_k, bias, scale, rel, drop, B, L_q, L_k, H, d)) return e;
     if (!aligned16(o)) return SIGATTN_ERR_MISALIGNED;
@@ -181,6 +196,11 @@ int forward(const void *q, const void *k, const void *v, void *o, const int32_t 
     p.bias = bias; p.scale = scale; p.B = B; p.H = H;
     const Extra x = extra(rel, drop);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (rel && !drop && L_q <= few::MOST) {
+        const size_t need = few_bytes(B, L_q, L_k, H, d);
+        const bool parts = need > 0 && workspace && workspace_bytes >= need && aligned16(workspace);
+        return few::launch(few::Few{p, x, parts ? few_splits(B, L_k, H) : 1, static_cast<float *>(workspace)}, d, s);
+    }
     return rel && drop ? mod::fwd_rel_dropout(p, x, d, s) : rel ? mod::fwd_rel(p, x, d, s) : mod::fwd_dropout(p, x, d, s);
 }
 
@@ -263,17 +283,19 @@ int sigmoid_attn_rel_buckets(int32_t *buckets, int num_buckets, int reach) {
     return SIGATTN_OK;
 }
 
+size_t sigmoid_attn_rel_fwd_workspace_bytes(int B, int L_q, int L_k, int H, int d) { return few_bytes(B, L_q, L_k, H, d); }
+
 int sigmoid_attn_rel_fwd(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k,
                          const float *bias, float scale, const void *table, const int32_t *buckets, int num_buckets, int reach,
-                         const int32_t *q_start, int B, int L_q, int L_k, int H, int d, void *stream) {
+                         const int32_t *q_start, int B, int L_q, int L_k, int H, int d, void *workspace, size_t workspace_bytes, void *stream) {
     const Bias rel{table, buckets, num_buckets, reach, q_start};
-    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, &rel, nullptr, B, L_q, L_k, H, d, stream);
+    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, &rel, nullptr, B, L_q, L_k, H, d, workspace, workspace_bytes, stream);
 }
 
 int sigmoid_attn_dropout_fwd(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k,
                              const float *bias, float scale, float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream) {
     const Drop drop{p, rng};
-    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, nullptr, &drop, B, L_q, L_k, H, d, stream);
+    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, nullptr, &drop, B, L_q, L_k, H, d, nullptr, 0, stream);
 }
 
 int sigmoid_attn_rel_dropout_fwd(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k,
@@ -281,7 +303,7 @@ int sigmoid_attn_rel_dropout_fwd(const void *q, const void *k, const void *v, vo
                                  const int32_t *q_start, float p, const uint64_t *rng, int B, int L_q, int L_k, int H, int d, void *stream) {
     const Bias rel{table, buckets, num_buckets, reach, q_start};
     const Drop drop{p, rng};
-    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, &rel, &drop, B, L_q, L_k, H, d, stream);
+    return forward(q, k, v, o, seqlens_q, seqlens_k, bias, scale, &rel, &drop, B, L_q, L_k, H, d, nullptr, 0, stream);
 }
 
 size_t sigmoid_attn_rel_bwd_workspace_bytes(int B, int L_q, int L_k, int H, int d, int reach) { return rel_bytes(B, L_q, L_k, H, d, reach); }

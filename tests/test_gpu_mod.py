@@ -122,6 +122,9 @@ SMALL = [
     (1, 257, 129, 2, (257,), (129,), 0, 1, (1000,)),
     (2, 129, 321, 1, (129, 128), (320, 321), 1, 3, (-1000000, 17)),
     (1, 513, 513, 1, (513,), (513,), 128, 32, None),
+    (2, 5, 3000, 1, (5, 3), (2999, 2047), 500, 64, (2994, 0)),
+    (3, 8, 131, 3, (8, 7, 0), (131, 128, 5), 30, 12, (123, -4, 0)),
+    (2, 2, 64, 2, (2, 1), (0, 64), 3, 5, None),
     (70, 65, 65, 1, [65 - i % 66 for i in range(70)], [65 - i % 66 for i in range(70)], 20, 41, None),
 ]
 
