@@ -49,7 +49,7 @@ torch = _Torch()
 
 
 class _NoFastCalls:
-    fwd = bwd = staticmethod(lambda *args: None)
+    fwd = bwd = mod_fwd = mod_bwd = staticmethod(lambda *args: None)
 
 
 def _fastcalls():
@@ -65,6 +65,10 @@ def _fastcalls():
         else:
             fast.use(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
                 lib.sigmoid_attn_fwd, lib.sigmoid_attn_bwd, lib.sigmoid_attn_bwd_onepass_workspace_bytes)))
+            fast.use_mod(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+                lib.sigmoid_attn_rel_fwd, lib.sigmoid_attn_dropout_fwd, lib.sigmoid_attn_rel_dropout_fwd, lib.sigmoid_attn_rel_bwd,
+                lib.sigmoid_attn_dropout_bwd, lib.sigmoid_attn_rel_dropout_bwd, lib.sigmoid_attn_rel_fwd_workspace_bytes,
+                lib.sigmoid_attn_rel_bwd_workspace_bytes)))
             _fast = fast
     return _fast
 
@@ -528,34 +532,58 @@ def sigmoid_attn_rel_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, tabl
     """Forward pass with table[buckets[clamp(j - i - q_start, -reach, reach) + reach]][h] added to the scores.
     table: bf16 [num_buckets, H]; buckets: int32 [2 * reach + 1] (sigmoid_attn_rel_buckets makes one); q_start: int32 [B] or None.
     The workspace (for up to eight queries against a long context) is allocated if None; an empty tensor stands for none."""
+    if out is None and workspace is None and stream is None:
+        res = (_fast or _fastcalls()).mod_fwd(1, q, k, v, seqlens_q, seqlens_k, bias, scale, table, buckets, q_start)
+        if res is not None:
+            return res
     return _mod_fwd("sigmoid_attn_rel_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), None, out, workspace, stream)
 
 
 def sigmoid_attn_rel_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, dq=None, dk=None, dv=None,
                          dtable=None, workspace=None, stream=None) -> Tuple:
     """(dQ, dK, dV, dtable) of sigmoid_attn_rel_fwd.  Outputs and the workspace are allocated if None."""
+    if dq is None and dk is None and dv is None and dtable is None and workspace is None and stream is None:
+        res = (_fast or _fastcalls()).mod_bwd(1, q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, table, buckets, q_start)
+        if res is not None:
+            return res
     return _mod_bwd("sigmoid_attn_rel_bwd", q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), None, dq, dk, dv, dtable,
                     workspace, stream)
 
 
 def sigmoid_attn_dropout_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, p: float, rng, out=None, stream=None):
     """Forward pass with dropout of the attention weights.  rng: int64 [2] in device memory, seed and offset."""
+    if out is None and stream is None:
+        res = (_fast or _fastcalls()).mod_fwd(2, q, k, v, seqlens_q, seqlens_k, bias, scale, p, rng)
+        if res is not None:
+            return res
     return _mod_fwd("sigmoid_attn_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, None, (p, rng), out, None, stream)
 
 
 def sigmoid_attn_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, p: float, rng, dq=None, dk=None, dv=None, stream=None) -> Tuple:
     """(dQ, dK, dV) of sigmoid_attn_dropout_fwd with the same p, seed and offset."""
+    if dq is None and dk is None and dv is None and stream is None:
+        res = (_fast or _fastcalls()).mod_bwd(2, q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, p, rng)
+        if res is not None:
+            return res
     return _mod_bwd("sigmoid_attn_dropout_bwd", q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, None, (p, rng), dq, dk, dv, None, None, stream)
 
 
 def sigmoid_attn_rel_dropout_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, table, buckets, p: float, rng, q_start=None, out=None,
                                  stream=None):
     """Forward pass with the relative position bias and dropout."""
+    if out is None and stream is None:
+        res = (_fast or _fastcalls()).mod_fwd(3, q, k, v, seqlens_q, seqlens_k, bias, scale, table, buckets, q_start, p, rng)
+        if res is not None:
+            return res
     return _mod_fwd("sigmoid_attn_rel_dropout_fwd", q, k, v, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), (p, rng), out, None, stream)
 
 
 def sigmoid_attn_rel_dropout_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, p: float, rng, q_start=None, dq=None,
                                  dk=None, dv=None, dtable=None, workspace=None, stream=None) -> Tuple:
     """(dQ, dK, dV, dtable) of sigmoid_attn_rel_dropout_fwd."""
+    if dq is None and dk is None and dv is None and dtable is None and workspace is None and stream is None:
+        res = (_fast or _fastcalls()).mod_bwd(3, q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, table, buckets, q_start, p, rng)
+        if res is not None:
+            return res
     return _mod_bwd("sigmoid_attn_rel_dropout_bwd", q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, (table, buckets, q_start), (p, rng), dq, dk, dv,
                     dtable, workspace, stream)

@@ -953,7 +953,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     // nobody reads before it is written again: the rows of it that this wave itself writes are the wave's scratch.
     auto sums = [&](auto slot) {
         if constexpr (Mod::SUMMED) {
-            static_assert(LD1 * 2 * (64 / C::CH) >= 1024 + 2 * (C::LM1 == 2 ? 8 : 0) && LD2 * 2 * (64 / C::CH) >= 1024 && C::LM2 == 0 && C::PER == 2, "scratch");
+            static_assert(LD1 * 2 * (64 / C::CH) >= 1024 + 2 * (C::LM1 == 2 ? 8 : 0) && LD2 * 2 * (64 / C::CH) >= 1024 && C::LM2 == 0 && C::PER >= 2, "scratch");
             const int own = wave * (64 / C::CH), row = slot.get() * BN + own;
             mod.sum(reinterpret_cast<unsigned char *>(y1s + row * LD1 + lds_shift<C::LM1>(own)), RPI * LD1 * 2,
                     reinterpret_cast<unsigned char *>(y2s + row * LD2), RPI * LD2 * 2, dsbuf[0][0], dsbuf[1][0]);

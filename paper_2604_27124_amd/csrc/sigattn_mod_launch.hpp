@@ -20,8 +20,8 @@ __global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod(const Params p, cons
     run_pass<MODE, D, QB, NW, 64, LD1, LD2, RING, false, M>(p, map_work<C::BM, C::THREADS>(p, blockIdx.x, s.map), smem, nullptr, M(p, x, s.ring));
 }
 
-// d = 64: both passes of the backward in one launch, as in sigattn_bwd_kernel.
-template <int D, int NW, int LD, int OCC, int RING_KV, int RING_Q, bool BIAS, bool DROP>
+// Both passes of the backward in one launch, as in sigattn_bwd_kernel (d = 64) and sigattn_half_bwd (d = 128).
+template <int D, int NW, int LD, int LD_Q, int OCC, int RING_KV, int RING_Q, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod_bwd(const Params kv, const Params q, const Extra x, const int q_first, const int first_tiles) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     __shared__ Scratch s;
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(NW * 64, OCC) sigattn_mod_bwd(const Params kv,
         w = is_kv ? map_work<C::BM, C::THREADS>(kv, rest, s.map) : map_work<C::BM, C::THREADS>(q, rest, s.map);
     }
     if (is_kv) run_pass<DKDV, D, 1, NW, 64, LD, LD, RING_KV, false, MK>(kv, w, smem, nullptr, MK(kv, x, s.ring));
-    else run_pass<DQ, D, 1, NW, 64, LD, LD, RING_Q, false, MQ>(q, w, smem, nullptr, MQ(q, x, s.ring));
+    else run_pass<DQ, D, 1, NW, 64, LD, LD_Q, RING_Q, false, MQ>(q, w, smem, nullptr, MQ(q, x, s.ring));
 }
 
 template <int MODE, int D, int QB, int NW, int LD1, int LD2, int OCC, int RING, bool BIAS, bool DROP>
@@ -57,26 +57,36 @@ int launch_pass(Params p, const Extra &x, hipStream_t stream) {
     return enqueue(sigattn_mod<MODE, D, QB, NW, LD1, LD2, OCC, RING, BIAS, DROP>, wgs, C::THREADS, C::LDS_BYTES, stream, p, x);
 }
 
+template <int D, int NW, int LD, int LD_Q, int OCC, int RING_KV, int RING_Q, bool BIAS, bool DROP>
+int launch_joint(Params kv, Params q, const Extra &x, hipStream_t stream) {
+    using C = Cfg<DKDV, D, 1, NW, 64, LD, LD, RING_KV>;
+    using CQ = Cfg<DQ, D, 1, NW, 64, LD, LD_Q, RING_Q>;
+    static_assert(C::BM == CQ::BM, "one tile height for both passes");
+    const long long kv_tiles = tiles_of<C>(kv), q_tiles = tiles_of<C>(q);
+    kv.in_order = q.in_order = batch_order(kv, kv_tiles + q_tiles, C::BM) || batch_order(q, kv_tiles + q_tiles, C::BM);
+    const int q_first = kv.N_str < q.N_str;                    // the pass whose workgroups stream more rows starts
+    return enqueue(sigattn_mod_bwd<D, NW, LD, LD_Q, OCC, RING_KV, RING_Q, BIAS, DROP>, kv_tiles + q_tiles, C::THREADS,
+                   C::LDS_BYTES > CQ::LDS_BYTES ? C::LDS_BYTES : CQ::LDS_BYTES, stream, kv, q, x, q_first, (int)(q_first ? q_tiles : kv_tiles));
+}
+
+// The shapes, and the rules that choose them, are those of the plain calls; d = 64 has an operand ring of four in dK/dV too, which
+// leaves the generator its registers.
+inline long long tiles128(const Params &p) { return ((long long)p.N + 127) / 128 * p.B * p.H; }
+
 template <bool BIAS, bool DROP>
 int launch_fwd(const Params &p, const Extra &x, int d, hipStream_t stream) {
     if (d == 64) {
         if (p.N <= 128 || (long long)p.B * p.H * ((p.N + 255) / 256) <= 256) return launch_pass<FWD, 64, 1, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
         return launch_pass<FWD, 64, 2, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
     }
+    if (tiles128(p) <= 256) return launch_pass<FWD, 128, 1, 4, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
     return launch_pass<FWD, 128, 1, 8, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
 }
 
 template <bool BIAS, bool DROP>
-int launch_bwd(Params kv, Params q, const Extra &x, int d, hipStream_t stream) {
-    if (d == 64) {
-        using C = Cfg<DKDV, 64, 1, 4, 64, 72, 72, 4>;
-        static_assert(C::LDS_BYTES == Cfg<DQ, 64, 1, 4, 64, 72, 72, 4>::LDS_BYTES, "one LDS size for both passes");
-        const long long kv_tiles = tiles_of<C>(kv), q_tiles = tiles_of<C>(q);
-        kv.in_order = q.in_order = batch_order(kv, kv_tiles + q_tiles, C::BM) || batch_order(q, kv_tiles + q_tiles, C::BM);
-        const int q_first = kv.N_str < q.N_str;                // the pass whose workgroups stream more rows starts
-        return enqueue(sigattn_mod_bwd<64, 4, 72, 2, 4, 4, BIAS, DROP>, kv_tiles + q_tiles, C::THREADS, C::LDS_BYTES, stream, kv, q, x, q_first,
-                       (int)(q_first ? q_tiles : kv_tiles));
-    }
+int launch_bwd(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream) {
+    if (d == 64) return launch_joint<64, 4, 72, 72, 2, 4, 4, BIAS, DROP>(kv, q, x, stream);
+    if (tiles128(kv) + tiles128(q) <= 512) return launch_joint<128, 4, 144, 136, 1, 4, 4, BIAS, DROP>(kv, q, x, stream);
     if (const int e = launch_pass<DKDV, 128, 1, 4, 144, 144, 1, 4, BIAS, DROP>(kv, x, stream)) return e;
     return launch_pass<DQ, 128, 1, 8, 144, 136, 1, 4, BIAS, DROP>(q, x, stream);
 }
