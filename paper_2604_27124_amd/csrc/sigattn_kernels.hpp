@@ -765,7 +765,11 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     // (a quarter of a tile earlier), which only the d = 128 forward pass gains from (12 x 1537 rows, H = 16: 172 -> 167 us;
     // d = 64, N = 8192, forward + backward 1543 -> 1559 us).
     constexpr bool LOAD_EARLY = MODE == FWD && D == 128;
-    auto step = [&](auto has_prev_c, auto has_next_c, auto drain_c, auto nb_c, auto slot, auto store_at_c, const int store_slot) {
+    // cb of the block whose sigmoid is made.  BIASED: scores of a tile whose pairs all have one bias start from zeros, and the
+    // bias rides on cb like that of the sequence; the sums of dS / cb are rescaled where it changes.
+    float cb_now = cb;
+    auto step = [&](auto has_prev_c, auto has_next_c, auto drain_c, auto nb_c, auto slot, auto store_at_c, const int store_slot, auto near_c) {
+        constexpr bool START = Mod::BIASED && decltype(near_c)::value;   // the next block's score tile starts from values in LDS
         constexpr int STORE_AT = decltype(store_at_c)::value;   // slot before which the staged tile goes to LDS (-1: never)
         constexpr bool HAS_PREV = decltype(has_prev_c)::value;  // a block went before: its output contractions
         constexpr bool HAS_NEXT = decltype(has_next_c)::value;  // a block follows: compute its scores
@@ -785,7 +789,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 if constexpr (!DRAIN) mod.template slot<k, SLOTS>();
             }
             if constexpr (Mod::BIASED) {
-                if constexpr (HAS_NEXT && !DRAIN && k == 0) {
+                if constexpr (HAS_NEXT && !DRAIN && k == 0 && !START) mod.advance();
+                if constexpr (HAS_NEXT && !DRAIN && k == 0 && START) {
                     static_for<0, QB>([&](auto q_) { mod.template start<decltype(q_)::value>(sbuf[PAR ^ 1][decltype(q_)::value]); });
                     mod.advance();
                 }
@@ -809,7 +814,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                     constexpr int ks = Order::ks(j), which = Order::which(j);
                     if constexpr (which == 0)
                         sbuf[PAR ^ 1][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            ring[(G0 + pos) % RING], xa[qb][ks], ks == 0 && !Mod::BIASED ? zero : sbuf[PAR ^ 1][qb], 0, 0, 0);
+                            ring[(G0 + pos) % RING], xa[qb][ks], ks == 0 && !START ? zero : sbuf[PAR ^ 1][qb], 0, 0, 0);
                     else
                         dbuf[PAR ^ 1][HAS2 ? qb : 0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                             ring[(G0 + pos) % RING], xb[HAS2 ? qb : 0][HAS2 ? ks : 0],
@@ -862,8 +867,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 constexpr IntC<1> B_{};
                 if constexpr (o == 0) s[ra] = __builtin_amdgcn_exp2f(s[ra]);
                 else if constexpr (o == 1) s[rb] = __builtin_amdgcn_exp2f(s[rb]);
-                else if constexpr (o == 2) set_y(A_, __builtin_fmaf(cb, s[ra], 1.0f));
-                else if constexpr (o == 3) set_y(B_, __builtin_fmaf(cb, s[rb], 1.0f));
+                else if constexpr (o == 2) set_y(A_, __builtin_fmaf(cb_now, s[ra], 1.0f));
+                else if constexpr (o == 3) set_y(B_, __builtin_fmaf(cb_now, s[rb], 1.0f));
                 else if constexpr (o == 4) set_y(A_, __builtin_amdgcn_rcpf(y_of(A_)));
                 else if constexpr (o == 5) set_y(B_, __builtin_amdgcn_rcpf(y_of(B_)));
                 else {
@@ -889,7 +894,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     using F_ = IntC<0>;
 
     // ---- prologue: tiles 0 and 1 of the stream into the ring, tile 2 into registers
-    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0);   // one owner tile a workgroup
+    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0, cb);   // one owner tile a workgroup
     {   // the first three tiles are requested back to back, so their latencies overlap
         load_tile();
         u32x4 a1[C::PER], a2[C::PER];
@@ -960,19 +965,34 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto tile_body = [&](auto slot_c) {            // from the second block of a tile through the first of the next
+    auto tile_body = [&](auto slot_c, auto near_c) {   // from the second block of a tile through the first of the next
         constexpr int slot = decltype(slot_c)::value;
         finish(IntC<0>{});
         static_for<1, NB>([&](auto nb_) {
-            if constexpr (decltype(nb_)::value + 1 < NB) step(T_{}, T_{}, F_{}, nb_, slot_c, NoStore{}, 0);
-            else step(T_{}, T_{}, F_{}, nb_, slot_c, StoreAt{}, (slot + 2) & (C::NBUF - 1));
+            if constexpr (decltype(nb_)::value + 1 < NB) step(T_{}, T_{}, F_{}, nb_, slot_c, NoStore{}, 0, near_c);
+            else step(T_{}, T_{}, F_{}, nb_, slot_c, StoreAt{}, (slot + 2) & (C::NBUF - 1), near_c);
         });
         asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(READS_AFTER) : "memory");
         if constexpr (!LOAD_EARLY) load_tile();
         finish(IntC<1>{});
         sums(IntC<(slot + 3) & (C::NBUF - 1)>{});      // the tile before this one; stored next: two steps on
-        step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0);
+        const float cb_before = cb_now;
+        if constexpr (Mod::BIASED) cb_now = mod.cb_of_tile();
+        step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0, near_c);
+        if constexpr (Mod::BIASED && HAS2) {
+            if (cb_now != cb_before) {                 // uniform
+                const float f = cb_before / cb_now;
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc0[qb][mb][i] *= f;
+                if constexpr (Mod::SUMMED) mod.rescale(f);
+            }
+        }
     };
+
     // P and dS of the streamed rows behind the valid length, in block nb of the last tile: exact zeros, as packed for the
     // output contractions.  Against a finite owner row they would add zeros anyway (the rows are zeros in LDS), but an Inf
     // in the owner row makes their scores 0 x Inf = NaN.  Two instructions a mask and one or two to apply it, on eight
@@ -1018,7 +1038,12 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         {
             const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if constexpr (Mod::BIASED) {
-                static_for<0, QB>([&](auto q_) { mod.template start<decltype(q_)::value>(sbuf[0][decltype(q_)::value]); });
+                const bool near = mod.next_tile();
+                static_for<0, QB>([&](auto q_) {
+                    constexpr int qb = decltype(q_)::value;
+                    if (near) mod.template start<qb>(sbuf[0][qb]);
+                    else sbuf[0][qb] = zero;
+                });
                 mod.advance();
             }
 #pragma unroll
@@ -1039,14 +1064,45 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         static_for<0, RING - 1>([&](auto J_) {
             if constexpr (Order::score(decltype(J_)::value)) ring[decltype(J_)::value % RING] = fetch(J_, DynInt{slot_rt}, IntC<0>{});
         });
-        step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0);
+        if constexpr (Mod::BIASED) {
+            cb_now = mod.cb_of_tile();
+            if (mod.near()) step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, T_{});
+            else step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, F_{});
+        } else {
+            step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, F_{});
+        }
 
         int t = ntiles - 1;
-        while (t > 0) {
-            if (slot_rt == 0) { tile_body(IntC<0>{}); slot_rt = 1; --t; }
-            if (t > 0 && slot_rt == 1) { tile_body(IntC<1>{}); slot_rt = 2; --t; }
-            if (t > 0 && slot_rt == 2) { tile_body(IntC<2>{}); slot_rt = 3; --t; }
-            if (t > 0 && slot_rt == 3) { tile_body(IntC<3>{}); slot_rt = 0; --t; }
+        if constexpr (Mod::BIASED) {
+            // Tiles of one kind follow each other (one far side, near, the other far side), so each kind has a loop of its own: with both
+            // kinds side by side in one loop the kernels kept 500 to 1800 bytes in scratch.
+            mod.next_tile();
+            auto run = [&](auto near_c) {
+                constexpr bool NEAR = decltype(near_c)::value;
+                auto go = [&](auto slot_c) {
+                    tile_body(slot_c, near_c);
+                    slot_rt = (decltype(slot_c)::value + 1) & (C::NBUF - 1);
+                    --t;
+                    mod.next_tile();
+                };
+                while (t > 0 && mod.near() == NEAR) {
+                    if (slot_rt == 0) go(IntC<0>{});
+                    if (t > 0 && mod.near() == NEAR && slot_rt == 1) go(IntC<1>{});
+                    if (t > 0 && mod.near() == NEAR && slot_rt == 2) go(IntC<2>{});
+                    if (t > 0 && mod.near() == NEAR && slot_rt == 3) go(IntC<3>{});
+                }
+            };
+            while (t > 0) {
+                run(F_{});
+                run(T_{});
+            }
+        } else {
+            while (t > 0) {
+                if (slot_rt == 0) { tile_body(IntC<0>{}, F_{}); slot_rt = 1; --t; }
+                if (t > 0 && slot_rt == 1) { tile_body(IntC<1>{}, F_{}); slot_rt = 2; --t; }
+                if (t > 0 && slot_rt == 2) { tile_body(IntC<2>{}, F_{}); slot_rt = 3; --t; }
+                if (t > 0 && slot_rt == 3) { tile_body(IntC<3>{}, F_{}); slot_rt = 0; --t; }
+            }
         }
 
         // ---- last tile.  The owner rows are not needed any more: request those of the next owner tile.
@@ -1060,13 +1116,13 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             mask_block(IntC<0>{});
             finish(IntC<0>{});
             static_for<1, NB>([&](auto nb_) {
-                step(T_{}, IntC<(decltype(nb_)::value + 1 < NB) ? 1 : 0>{}, F_{}, nb_, slot, NoStore{}, 0);
+                step(T_{}, IntC<(decltype(nb_)::value + 1 < NB) ? 1 : 0>{}, F_{}, nb_, slot, NoStore{}, 0, F_{});
                 mask_block(nb_);
                 finish(nb_);
             });
             sums(DynInt{(slot_rt + 2) & (C::NBUF - 1)});   // no tile of its own: last read before the barrier behind the tile before
             const DynInt slot_next{(slot_rt + 1) & (C::NBUF - 1)};
-            step(T_{}, F_{}, T_{}, IntC<0>{}, slot_next, NoStore{}, 0);
+            step(T_{}, F_{}, T_{}, IntC<0>{}, slot_next, NoStore{}, 0, F_{});
             if (more) {
                 store_tile((slot_rt + 2) & (C::NBUF - 1));
                 load_tile();
@@ -1093,7 +1149,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             }
         }
 
-        if constexpr (Mod::SUMMED) mod.close();
+        if constexpr (Mod::SUMMED) mod.close(cb_now / cb);
 
         // ---- epilogue: transposed fp32 accumulators -> bf16 rows.  Lane (c, g) holds owner row c of each block;
         // registers 4 q4 .. 4 q4 + 3 of output block mb hold head-dim columns out_col(mb, q4) + 4 g + 0..3 of the
@@ -1103,7 +1159,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         using TL_ACC0 = TrLayout<(MODE == FWD) ? C::LM2 : C::LM1>;      // FWD contracts V^T; DQ K^T; DKDV Q^T (acc0), dO^T (acc1)
         using TL_ACC1 = TrLayout<C::LM2>;
         const float used = Mod::SIFTED ? mod.scale() : 1.0f;            // of the weights
-        const float oscale = used * ((MODE == FWD) ? 1.0f : p.scale * cb);   // dQ and dK carry the factor `scale`; their sums are over dS / cb
+        const float oscale = used * ((MODE == FWD) ? 1.0f : p.scale * cb_now);   // dQ and dK carry the factor `scale`; their sums are over dS / cb
         auto chunk = [&](const f32x16 &a, const int pr, const float f) {   // columns of q4 = 2 pr + g
             const unsigned e0 = pack_bf16(a[8 * pr + 0] * f, a[8 * pr + 1] * f), e1 = pack_bf16(a[8 * pr + 2] * f, a[8 * pr + 3] * f);
             const unsigned o0 = pack_bf16(a[8 * pr + 4] * f, a[8 * pr + 5] * f), o1 = pack_bf16(a[8 * pr + 6] * f, a[8 * pr + 7] * f);

@@ -9,7 +9,9 @@
 // The bias depends on j - i alone.  Streamed rows pass an owner row in order, so the values that the score tiles of an owner
 // tile start from (the accumulators of the score contraction: no vector instruction adds them) are a window of one vector
 // over the distances, which moves on by 64 entries a tile.  It lives in a ring in LDS; a tile's new entries are looked up
-// (bucket, then table) a tile ahead of each other and stored with the tile.  Any reach costs the same.
+// (bucket, then table) a tile ahead of each other and stored with the tile.  A tile whose pairs, for a wave, all lie at or beyond
+// +-reach has one bias: there the score tiles start from zeros and the bias is a factor of the constant that the bias of the
+// sequence is, for nothing.  us at B = 4, H = 12, N = 8192, reach 256, forward and backward: all tiles from the ring TODO, so TODO.
 #pragma once
 #include "sigattn_kernels.hpp"
 
@@ -75,6 +77,9 @@ struct Mods {
     int next_x, next_pos;                                      // chunk that is looked up next: distance of its entry 0, ring position
     int bucket;
     float value;
+    int tile_lo, above_from, below_to;                         // lowest distance of the tile in hand; where the far sides begin
+    bool near_tile;
+    float cb_base, cb_above, cb_below, cb_tile;
 
     // dropout
     unsigned keep, key0, key1, c3, c2, row, group;             // row, group: counter words of owner block 0, this block
@@ -102,7 +107,7 @@ struct Mods {
         return d > -n && d < ns ? v : 0.f;
     }
 
-    __device__ __forceinline__ void open(const int z, const int h_, const int n_, const int ns_, const int m0_) {
+    __device__ __forceinline__ void open(const int z, const int h_, const int n_, const int ns_, const int m0_, const float cb) {
         h = h_; n = n_; ns = ns_; m0 = m0_;
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -115,6 +120,19 @@ struct Mods {
             next_x = -m0;
             next_pos = BM & (RING - 1);
             bucket = bucket_at(next_x + lane);
+            // the far sides: where their bias is a factor that fp32 holds with room on both sides (-inf is a mask, and goes through the ring)
+            auto far_cb = [&](const int b) {
+                const int i = b < 0 ? 0 : (b >= x.num_buckets ? x.num_buckets - 1 : b);
+                const float f = cb * __builtin_amdgcn_exp2f((float)x.table[(size_t)i * p.H + h] * -1.4426950408889634f);
+                return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
+            };
+            cb_base = cb;
+            cb_above = far_cb(x.buckets[2 * x.reach]);
+            cb_below = far_cb(x.buckets[0]);
+            above_from = cb_above > 0x1p-100f && cb_above < 0x1p100f ? x.reach : 0x7FFFFFFF;
+            below_to = cb_below > 0x1p-100f && cb_below < 0x1p100f ? -x.reach : (int)0x80000000;
+            const int first_row = m0 + 32 * QB * wave;
+            tile_lo = MODE == DKDV ? first_row - 63 - start_pos + 64 : -first_row - (32 * QB - 1) - start_pos - 64;
         }
         if constexpr (DROP) {
             keep = __builtin_amdgcn_readfirstlane(x.keep);
@@ -139,6 +157,18 @@ struct Mods {
             below = 0.f;
         }
     }
+    // Goes on to the next tile; whether its scores start from the ring.
+    __device__ __forceinline__ bool next_tile() {
+        tile_lo += MODE == DKDV ? -64 : 64;
+        const bool above = tile_lo >= above_from, below = tile_lo + 32 * QB + 62 <= below_to;
+        const float a = cb_above, b = cb_below, c = cb_base;    // values: a choice between members would keep them all in memory
+        cb_tile = above ? a : (below ? b : c);
+        near_tile = !above && !below;
+        return near_tile;
+    }
+    __device__ __forceinline__ bool near() const { return near_tile; }
+    __device__ __forceinline__ float cb_of_tile() const { return cb_tile; }
+
     // The entries of the first two tiles and of the owner tile in front of them.
     __device__ __forceinline__ void fill() {
         for (int e = threadIdx.x; e < BM + 128; e += THREADS) {
@@ -366,10 +396,15 @@ struct Mods {
         sum_block(put, get, d0);
         sum_block(put, get, d1);
     }
+    // The unit of the sums, 1 / cb, changes by `f`.  (Near blocks lie in tiles of the same unit.)
+    __device__ __forceinline__ void rescale(const float f) {
+        if (!open_window) acc[0] *= f;
+    }
     // Behind the last block: what is left in the window, and the far sums (row 0 of the accumulators, lanes 0 to 15).
-    __device__ __forceinline__ void close() {
+    __device__ __forceinline__ void close(const float unit) {
         if (!active) return;
         if (open_window) { flush(); acc = f32x4{0.f, 0.f, 0.f, 0.f}; }
+        acc[0] *= unit;
         const bool all_below = k <= first;                     // not one block was near, or beyond
         float v = lane < 16 ? acc[0] : 0.f, u = lane < 16 ? below : 0.f;
 #pragma unroll

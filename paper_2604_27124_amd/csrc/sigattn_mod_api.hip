@@ -23,6 +23,36 @@ __device__ __forceinline__ int clamped(int v, int lo, int hi) { return v < lo ? 
 
 __device__ __forceinline__ int start_of(const Lengths &l, int z) { return l.start ? clamped(l.start[z], -(1 << 29), 1 << 29) : 0; }
 
+// Sum over the rows of a sequence that have entry `c` of chunk `chunk`: of 32 queries each, from row `first` on every `step`.
+__device__ __forceinline__ float sum_rows(const Lengths &l, const Extra &x, const int z, const int h, const int chunk, const int c, const bool far,
+                                          const int first, const int step, const int entries) {
+    const int blocks = (l.L_q + 31) / 32;
+    const size_t stride = (size_t)(entries + mod::FAR);
+    const int nq = clamped(l.q[z], 0, l.L_q), ns = clamped(l.k[z], 0, l.L_k);
+    if (nq == 0 || ns == 0) return 0.f;
+    const RowSums r(x.reach, start_of(l, z), blocks);
+    const int k = r.first + chunk, key_blocks = 2 * ((ns + 63) / 64);
+    // b = k + ob is a near block's, or b - 1 is (what the last near block leaves behind)
+    int from = -k, to = key_blocks - k;                                        // key blocks 0 .. key_blocks - 1
+    if (chunk > 0) ++to;                                                       // and the one behind, of diagonal k - 1
+    if (k > r.last) { ++from; if (k > r.last + 1 || chunk == 0) to = from; }   // only as what is left
+    const int all = (nq + 31) / 32;
+    if (far) { from = 0; to = c < 2 ? all : 0; }
+    from = from < 0 ? 0 : from;
+    to = to > all ? all : to;
+    const float *const rows = x.part + ((size_t)z * l.H + h) * blocks * stride + 32 * chunk + c;
+    float t = 0.f;
+    int ob = from + first;
+    for (; ob + 3 * step < to; ob += 4 * step) {                               // four loads in flight
+        const float a = rows[ob * stride], b = rows[(ob + step) * stride], e = rows[(ob + 2 * step) * stride], f = rows[(ob + 3 * step) * stride];
+        t += (a + b) + (e + f);
+    }
+    for (; ob < to; ob += step) t += rows[ob * stride];
+    // the rows are of dS / cb, without 1 / keep
+    const float cb = __builtin_amdgcn_exp2f(__builtin_fminf(__builtin_fmaxf(-l.bias[z] * 1.4426950408889634f, -126.0f), 126.0f));
+    return t * (cb * x.inv_keep);
+}
+
 // Sums over rows, in fixed order and without atomics.  Group s of `groups` takes sequences s, s + groups, ...: [group][H][entries + FAR].  A
 // workgroup takes 32 entries of a head; of its eight groups of 32 lanes `seqs` take a sequence each, and the others share the
 // rows of these.
@@ -31,34 +61,11 @@ __global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const E
     const int entries = RowSums::entries(x.reach, l.L_q, l.L_k), chunks = entries / 32 + 1;
     const int chunk = blockIdx.x % chunks, rest = blockIdx.x / chunks, h = rest % l.H, group = rest / l.H;
     const int c = threadIdx.x & 31, mine = threadIdx.x >> 5, step = 8 / seqs;
-    const int blocks = (l.L_q + 31) / 32;
     const bool far = chunk == chunks - 1;
     const size_t stride = (size_t)(entries + mod::FAR);
     float total = 0.f;
-    for (long long z = group + (long long)groups * (mine % seqs); z < l.B; z += (long long)groups * seqs) {
-        const int nq = clamped(l.q[z], 0, l.L_q), ns = clamped(l.k[z], 0, l.L_k);
-        if (nq == 0 || ns == 0) continue;
-        const RowSums r(x.reach, start_of(l, z), blocks);
-        const int k = r.first + chunk, key_blocks = 2 * ((ns + 63) / 64);
-        // rows that have the entry: b = k + ob is a near block's, or b - 1 is (what the last near block leaves behind)
-        int from = -k, to = key_blocks - k;                                    // key blocks 0 .. key_blocks - 1
-        if (chunk > 0) ++to;                                                   // and the one behind, of diagonal k - 1
-        if (k > r.last) { ++from; if (k > r.last + 1 || chunk == 0) to = from; }   // only as what is left
-        const int all = (nq + 31) / 32;
-        if (far) { from = 0; to = c < 2 ? all : 0; }
-        from = from < 0 ? 0 : from;
-        to = to > all ? all : to;
-        const float *const rows = x.part + ((size_t)z * l.H + h) * blocks * stride + 32 * chunk + c;
-        float t = 0.f;
-        int ob = from + mine / seqs;
-        for (; ob + 3 * step < to; ob += 4 * step) {                           // four loads in flight
-            const float a = rows[ob * stride], b = rows[(ob + step) * stride], e = rows[(ob + 2 * step) * stride], f = rows[(ob + 3 * step) * stride];
-            t += (a + b) + (e + f);
-        }
-        for (; ob < to; ob += step) t += rows[ob * stride];
-        const float cb = __builtin_amdgcn_exp2f(__builtin_fminf(__builtin_fmaxf(-l.bias[z] * 1.4426950408889634f, -126.0f), 126.0f));
-        total += t * (cb * x.inv_keep);
-    }
+    for (long long z = group + (long long)groups * (mine % seqs); z < l.B; z += (long long)groups * seqs)
+        total += sum_rows(l, x, (int)z, h, chunk, c, far, mine / seqs, step, entries);
     s[mine][c] = total;
     __syncthreads();
     if (mine == 0) {
@@ -70,8 +77,10 @@ __global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const E
 }
 
 // dtable[b][h] for 16 buckets of a head: the entries of all groups (of one group where every sequence has a start of its own), a
-// thousand at a time, with their buckets, in LDS; each wave goes through them for its four buckets.
-constexpr int TABLE_BUCKETS = 16, TABLE_ENTRIES = 1024;
+// thousand at a time, with their buckets, in LDS; each wave goes through them for its four buckets.  DIRECT: a few rows,
+// taken as they are, without the launch above (B = 2, H = 2, N = 256: backward TODO -> TODO us); a group is a sequence then.
+constexpr int TABLE_BUCKETS = 16, TABLE_ENTRIES = 1024, DIRECT_ROWS = 64;
+template <bool DIRECT>
 __global__ void __launch_bounds__(256) sigattn_rel_table(const Lengths l, const Extra x, const int groups, bf16_t *dtable) {
     __shared__ float value[TABLE_ENTRIES];
     __shared__ int bucket[TABLE_ENTRIES];
@@ -92,8 +101,12 @@ __global__ void __launch_bounds__(256) sigattn_rel_table(const Lengths l, const 
                 bucket[i] = clamped(x.buckets[clamped(t, -x.reach, x.reach) + x.reach], 0, x.num_buckets - 1);
                 float v = 0.f;
                 int c = 0;
-                for (; c + 4 <= count; c += 4) v += (from[c * head + e] + from[(c + 1) * head + e]) + (from[(c + 2) * head + e] + from[(c + 3) * head + e]);
-                for (; c < count; ++c) v += from[c * head + e];
+                if (DIRECT) {
+                    for (; c < count; ++c) v += sum_rows(l, x, g + c, h, e / 32, e % 32, e >= entries, 0, 1, entries);
+                } else {
+                    for (; c + 4 <= count; c += 4) v += (from[c * head + e] + from[(c + 1) * head + e]) + (from[(c + 2) * head + e] + from[(c + 3) * head + e]);
+                    for (; c < count; ++c) v += from[c * head + e];
+                }
                 value[i] = v;
             }
             __syncthreads();
@@ -173,10 +186,11 @@ int few_splits(int B, int L_k, int H) {
     return s < 1 ? 1 : (int)s;
 }
 int few_rows(int L_q) { return L_q == 1 ? 1 : L_q == 2 ? 2 : L_q <= 4 ? 4 : 8; }
+int few_groups(int L_q) { return (L_q + 7) / 8; }
 size_t few_bytes(int B, int L_q, int L_k, int H, int d) {
     if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK || L_q > few::MOST) return 0;
     const int s = few_splits(B, L_k, H);
-    return s == 1 ? 0 : (size_t)s * B * H * few_rows(L_q) * d * sizeof(float);
+    return s == 1 ? 0 : (size_t)s * B * H * few_groups(L_q) * few_rows(L_q) * d * sizeof(float);
 }
 
 int forward(const void *q, const void *k, const void *v, void *o, const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
@@ -199,7 +213,7 @@ int forward(const void *q, const void *k, const void *v, void *o, const int32_t 
     if (rel && !drop && L_q <= few::MOST) {
         const size_t need = few_bytes(B, L_q, L_k, H, d);
         const bool parts = need > 0 && workspace && workspace_bytes >= need && aligned16(workspace);
-        return few::launch(few::Few{p, x, parts ? few_splits(B, L_k, H) : 1, static_cast<float *>(workspace)}, d, s);
+        return few::launch(few::Few{p, x, parts ? few_splits(B, L_k, H) : 1, few_groups(L_q), static_cast<float *>(workspace)}, d, s);
     }
     return rel && drop ? mod::fwd_rel_dropout(p, x, d, s) : rel ? mod::fwd_rel(p, x, d, s) : mod::fwd_dropout(p, x, d, s);
 }
@@ -253,8 +267,9 @@ int backward(const void *q, const void *k, const void *v, const void *d_o, void 
     x.by_distance = x.part + row_floats(B, L_q, L_k, H, rel->reach);
     if (int e = drop ? mod::bwd_rel_dropout(pk, pq, x, d, s) : mod::bwd_rel(pk, pq, x, d, s)) return e;
     const Lengths l{seqlens_q, seqlens_k, rel->q_start, bias, L_q, L_k, H, B};
+    if ((long long)B * ((L_q + 31) / 32) <= DIRECT_ROWS) return enqueue(sigattn_rel_table<true>, table_wgs, 256, 0, s, l, x, B, static_cast<bf16_t *>(dtable));
     if (int e = enqueue(sigattn_rel_rows, row_wgs, 256, 0, s, l, x, groups, seqs)) return e;
-    return enqueue(sigattn_rel_table, table_wgs, 256, 0, s, l, x, groups, static_cast<bf16_t *>(dtable));
+    return enqueue(sigattn_rel_table<false>, table_wgs, 256, 0, s, l, x, groups, static_cast<bf16_t *>(dtable));
 }
 
 }  // namespace

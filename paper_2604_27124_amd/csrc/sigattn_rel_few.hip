@@ -7,7 +7,7 @@ namespace few {
 
 template <int D, int R>
 static int run(const Few &f, hipStream_t stream) {
-    const long long heads = (long long)f.p.B * f.p.H;
+    const long long heads = (long long)f.p.B * f.p.H * f.groups;
     if (const int e = enqueue(sigattn_rel_few<D, R>, heads * f.splits, THREADS, 0, stream, f)) return e;
     if (f.splits == 1) return SIGATTN_OK;
     return enqueue(sigattn_rel_few_join<D, R>, (heads * (R * D) + 255) / 256, 256, 0, stream, f);

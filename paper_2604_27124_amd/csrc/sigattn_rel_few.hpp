@@ -1,4 +1,4 @@
-// Forward pass with a relative position bias for up to eight queries a sequence: single tokens against a long context.
+// Forward pass with a relative position bias for up to 16 queries a sequence: single tokens against a long context.
 //
 // Every key and value is used by few queries, so the call is bound by reading them once, and matrix instructions, which take
 // 32 queries at a time, would mostly multiply padding.  A wave reads whole rows (d = 64: eight lanes of 16 bytes a row, eight rows a load; d = 128: 16 and
@@ -14,7 +14,7 @@
 namespace sigattn {
 namespace few {
 
-constexpr int NW = 8, THREADS = 64 * NW, MOST = 8;             // most: queries of a sequence
+constexpr int NW = 8, THREADS = 64 * NW, MOST = 16;            // most: queries of a sequence, in groups of eight
 constexpr int CHUNK = 2048;                                    // keys whose bias is in LDS
 
 template <int CTRL>
@@ -45,17 +45,17 @@ __device__ __forceinline__ float dot(const u32x4 a, const u32x4 b) {
 struct Few {
     Params p;                        // q, k, v, out0, seqlens (queries), seqlens_str (keys), bias, scale, B, N, N_str, H
     mod::Extra x;
-    int splits;
-    float *part;                     // [splits][B][H][R][D] where there are several
+    int splits, groups;              // parts of the keys; groups of R queries
+    float *part;                     // [splits][B][H][groups][R][D] where there are several
 };
 
 template <int D, int R>
 __global__ void __launch_bounds__(THREADS, 2) sigattn_rel_few(const Few f) {
     constexpr int LANES = D / 8, ROWS = 64 / LANES, U = 4, STEP = ROWS * U;        // lanes of a row; rows of a load; loads; keys of a wave's step
-    __shared__ float bias[CHUNK + MOST];
+    __shared__ float bias[CHUNK + R];
     __shared__ float red[NW][R][D];
     const Params &p = f.p;
-    const int zh = blockIdx.x / f.splits, split = blockIdx.x % f.splits, z = zh / p.H, h = zh % p.H;
+    const int zhg = blockIdx.x / f.splits, split = blockIdx.x % f.splits, zh = zhg / f.groups, r0 = zhg % f.groups * R, z = zh / p.H, h = zh % p.H;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane % LANES, row = lane / LANES;
     int nq = p.seqlens[z], ns = p.seqlens_str[z];
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_rel_few(const Few f) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         q[r] = u32x4{0u, 0u, 0u, 0u};
-        if (r < nq) q[r] = *reinterpret_cast<const u32x4 *>(p.q + ((size_t)z * p.N + r) * stride + (size_t)h * D + 8 * col);
+        if (r0 + r < nq) q[r] = *reinterpret_cast<const u32x4 *>(p.q + ((size_t)z * p.N + r0 + r) * stride + (size_t)h * D + 8 * col);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[r][e] = 0.f;
     }
@@ -86,8 +86,8 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_rel_few(const Few f) {
     for (long long base = k_lo; base < k_hi; base += CHUNK) {
         const int count = (int)(k_hi - base < CHUNK ? k_hi - base : CHUNK);
         __syncthreads();
-        for (int e = threadIdx.x; e < count + R - 1; e += THREADS) {           // entry e: distance (base + e - (R - 1)) - start
-            const int j = (int)base + e - (R - 1);
+        for (int e = threadIdx.x; e < count + R - 1; e += THREADS) {           // entry e: distance base + e - (R - 1) - r0 - start
+            const int j = (int)base + e - (R - 1) - r0;
             int t = j - start;
             t = t < -f.x.reach ? -f.x.reach : (t > f.x.reach ? f.x.reach : t);
             int b = f.x.buckets[t + f.x.reach];
@@ -156,8 +156,8 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_rel_few(const Few f) {
         float t = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) t += red[w][r][c];
-        if (f.splits > 1) f.part[(((size_t)split * p.B + z) * p.H + h) * (R * D) + e] = t;
-        else if (r < p.N) p.out0[((size_t)z * p.N + r) * stride + (size_t)h * D + c] = (bf16_t)(r < nq ? t : 0.f);
+        if (f.splits > 1) f.part[((size_t)split * p.B * p.H * f.groups + zhg) * (R * D) + e] = t;
+        else if (r0 + r < p.N) p.out0[((size_t)z * p.N + r0 + r) * stride + (size_t)h * D + c] = (bf16_t)(r0 + r < nq ? t : 0.f);
     }
 }
 
@@ -165,10 +165,10 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_rel_few(const Few f) {
 template <int D, int R>
 __global__ void __launch_bounds__(256) sigattn_rel_few_join(const Few f) {
     const Params &p = f.p;
-    const size_t all = (size_t)p.B * p.H * (R * D), at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t all = (size_t)p.B * p.H * f.groups * (R * D), at = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (at >= all) return;
-    const int r = (int)(at % (R * D)) / D, c = (int)(at % D);
-    const size_t zh = at / (R * D);
+    const size_t zhg = at / (R * D), zh = zhg / f.groups;
+    const int r = (int)(zhg % f.groups) * R + (int)(at % (R * D)) / D, c = (int)(at % D);
     const int z = (int)(zh / p.H), h = (int)(zh % p.H);
     int nq = p.seqlens[z];
     nq = nq < 0 ? 0 : (nq > p.N ? p.N : nq);

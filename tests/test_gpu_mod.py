@@ -125,6 +125,8 @@ SMALL = [
     (2, 5, 3000, 1, (5, 3), (2999, 2047), 500, 64, (2994, 0)),
     (3, 8, 131, 3, (8, 7, 0), (131, 128, 5), 30, 12, (123, -4, 0)),
     (2, 2, 64, 2, (2, 1), (0, 64), 3, 5, None),
+    (1, 13, 2500, 2, (11,), (2400,), 100, 32, (-3,)),
+    (2, 400, 700, 1, (400, 333), (700, 650), 30, 32, (100, -60)),
     (70, 65, 65, 1, [65 - i % 66 for i in range(70)], [65 - i % 66 for i in range(70)], 20, 41, None),
 ]
 
