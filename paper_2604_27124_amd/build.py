@@ -12,8 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsigattn.so")
-SOURCES = ["sigattn_api.hip", "sigattn_mod_api.hip", "sigattn_rel.hip", "sigattn_dropout.hip", "sigattn_rel_dropout.hip",
-           "sigattn_rel_few.hip"]
+SOURCES = ["sigattn_api.hip", "sigattn_mod_api.hip", "sigattn_rel_few.hip",
+           *(f"sigattn_{kind}_{d}.hip" for kind in ("rel_dropout", "rel", "dropout") for d in (64, 128))]
 PROBE_LIB = os.path.join(HERE, "libmachine_probes.so")  # measurement aids for the benchmark, a library of their own
 PROBE_SOURCES = ["machine_probes.hip"]
 

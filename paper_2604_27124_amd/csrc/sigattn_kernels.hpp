@@ -659,7 +659,6 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             st1[it] = __builtin_amdgcn_raw_buffer_load_b128(d1, (int)ld_off0, it * (int)pass_bytes, 0);
             st2[it] = __builtin_amdgcn_raw_buffer_load_b128(d2, (int)ld_off0, it * (int)pass_bytes, 0);
         }
-        if constexpr (Mod::BIASED) mod.request();
         next1 += (size_t)BN * row_stride;
         next2 += (size_t)BN * row_stride;
         rows_left = rows_left > BN ? rows_left - BN : 0;
@@ -765,8 +764,10 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     // (a quarter of a tile earlier), which only the d = 128 forward pass gains from (12 x 1537 rows, H = 16: 172 -> 167 us;
     // d = 64, N = 8192, forward + backward 1543 -> 1559 us).
     constexpr bool LOAD_EARLY = MODE == FWD && D == 128;
-    // cb of the block whose sigmoid is made.  BIASED: scores of a tile whose pairs all have one bias start from zeros, and the
-    // bias rides on cb like that of the sequence; the sums of dS / cb are rescaled where it changes.
+    // cb of the block whose sigmoid is made.  BIASED, forward: scores of a tile whose pairs all have one bias start from zeros, and the
+    // bias rides on cb like that of the sequence.
+    constexpr bool KINDS = Mod::BIASED && MODE == FWD;
+    using Near = IntC<Mod::BIASED ? 1 : 0>;
     float cb_now = cb;
     auto step = [&](auto has_prev_c, auto has_next_c, auto drain_c, auto nb_c, auto slot, auto store_at_c, const int store_slot, auto near_c) {
         constexpr bool START = Mod::BIASED && decltype(near_c)::value;   // the next block's score tile starts from values in LDS
@@ -976,21 +977,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         if constexpr (!LOAD_EARLY) load_tile();
         finish(IntC<1>{});
         sums(IntC<(slot + 3) & (C::NBUF - 1)>{});      // the tile before this one; stored next: two steps on
-        const float cb_before = cb_now;
-        if constexpr (Mod::BIASED) cb_now = mod.cb_of_tile();
+        if constexpr (KINDS) cb_now = mod.cb_of_tile();
         step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0, near_c);
-        if constexpr (Mod::BIASED && HAS2) {
-            if (cb_now != cb_before) {                 // uniform
-                const float f = cb_before / cb_now;
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc0[qb][mb][i] *= f;
-                if constexpr (Mod::SUMMED) mod.rescale(f);
-            }
-        }
     };
 
     // P and dS of the streamed rows behind the valid length, in block nb of the last tile: exact zeros, as packed for the
@@ -1038,7 +1026,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         {
             const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if constexpr (Mod::BIASED) {
-                const bool near = mod.next_tile();
+                bool near = true;
+                if constexpr (KINDS) near = mod.next_tile();
                 static_for<0, QB>([&](auto q_) {
                     constexpr int qb = decltype(q_)::value;
                     if (near) mod.template start<qb>(sbuf[0][qb]);
@@ -1064,18 +1053,17 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         static_for<0, RING - 1>([&](auto J_) {
             if constexpr (Order::score(decltype(J_)::value)) ring[decltype(J_)::value % RING] = fetch(J_, DynInt{slot_rt}, IntC<0>{});
         });
-        if constexpr (Mod::BIASED) {
+        if constexpr (KINDS) {
             cb_now = mod.cb_of_tile();
             if (mod.near()) step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, T_{});
             else step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, F_{});
         } else {
-            step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, F_{});
+            step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, Near{});
         }
 
         int t = ntiles - 1;
-        if constexpr (Mod::BIASED) {
-            // Tiles of one kind follow each other (one far side, near, the other far side), so each kind has a loop of its own: with both
-            // kinds side by side in one loop the kernels kept 500 to 1800 bytes in scratch.
+        if constexpr (KINDS) {
+            // Tiles of one kind follow each other (one far side, near, the other far side), so each kind has a loop of its own.
             mod.next_tile();
             auto run = [&](auto near_c) {
                 constexpr bool NEAR = decltype(near_c)::value;
@@ -1098,10 +1086,10 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             }
         } else {
             while (t > 0) {
-                if (slot_rt == 0) { tile_body(IntC<0>{}, F_{}); slot_rt = 1; --t; }
-                if (t > 0 && slot_rt == 1) { tile_body(IntC<1>{}, F_{}); slot_rt = 2; --t; }
-                if (t > 0 && slot_rt == 2) { tile_body(IntC<2>{}, F_{}); slot_rt = 3; --t; }
-                if (t > 0 && slot_rt == 3) { tile_body(IntC<3>{}, F_{}); slot_rt = 0; --t; }
+                if (slot_rt == 0) { tile_body(IntC<0>{}, Near{}); slot_rt = 1; --t; }
+                if (t > 0 && slot_rt == 1) { tile_body(IntC<1>{}, Near{}); slot_rt = 2; --t; }
+                if (t > 0 && slot_rt == 2) { tile_body(IntC<2>{}, Near{}); slot_rt = 3; --t; }
+                if (t > 0 && slot_rt == 3) { tile_body(IntC<3>{}, Near{}); slot_rt = 0; --t; }
             }
         }
 
@@ -1149,7 +1137,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             }
         }
 
-        if constexpr (Mod::SUMMED) mod.close(cb_now / cb);
+        if constexpr (Mod::SUMMED) mod.close();
 
         // ---- epilogue: transposed fp32 accumulators -> bf16 rows.  Lane (c, g) holds owner row c of each block;
         // registers 4 q4 .. 4 q4 + 3 of output block mb hold head-dim columns out_col(mb, q4) + 4 g + 0..3 of the
@@ -1159,7 +1147,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         using TL_ACC0 = TrLayout<(MODE == FWD) ? C::LM2 : C::LM1>;      // FWD contracts V^T; DQ K^T; DKDV Q^T (acc0), dO^T (acc1)
         using TL_ACC1 = TrLayout<C::LM2>;
         const float used = Mod::SIFTED ? mod.scale() : 1.0f;            // of the weights
-        const float oscale = used * ((MODE == FWD) ? 1.0f : p.scale * cb_now);   // dQ and dK carry the factor `scale`; their sums are over dS / cb
+        const float oscale = used * ((MODE == FWD) ? 1.0f : p.scale * cb);   // dQ and dK carry the factor `scale`; their sums are over dS / cb
         auto chunk = [&](const f32x16 &a, const int pr, const float f) {   // columns of q4 = 2 pr + g
             const unsigned e0 = pack_bf16(a[8 * pr + 0] * f, a[8 * pr + 1] * f), e1 = pack_bf16(a[8 * pr + 2] * f, a[8 * pr + 3] * f);
             const unsigned o0 = pack_bf16(a[8 * pr + 4] * f, a[8 * pr + 5] * f), o1 = pack_bf16(a[8 * pr + 6] * f, a[8 * pr + 7] * f);

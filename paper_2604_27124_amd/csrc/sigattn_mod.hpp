@@ -9,9 +9,9 @@
 // The bias depends on j - i alone.  Streamed rows pass an owner row in order, so the values that the score tiles of an owner
 // tile start from (the accumulators of the score contraction: no vector instruction adds them) are a window of one vector
 // over the distances, which moves on by 64 entries a tile.  It lives in a ring in LDS; a tile's new entries are looked up
-// (bucket, then table) a tile ahead of each other and stored with the tile.  A tile whose pairs, for a wave, all lie at or beyond
-// +-reach has one bias: there the score tiles start from zeros and the bias is a factor of the constant that the bias of the
-// sequence is, for nothing.  us at B = 4, H = 12, N = 8192, reach 256, forward and backward: all tiles from the ring TODO, so TODO.
+// (bucket, then table) a tile ahead of each other and stored with the tile.  In the forward pass a tile whose pairs, for a wave, all lie at
+// or beyond +-reach starts from zeros, and its one bias is a factor of the constant that the bias of the sequence is.  (B = 4, H = 12,
+// N = 8192, reach 256: TODO us, with all tiles from the ring TODO.  The backward passes gain 1 % by it, for twice the code.)
 #pragma once
 #include "sigattn_kernels.hpp"
 
@@ -74,9 +74,9 @@ struct Mods {
 
     // bias
     unsigned at;                                               // byte in the ring of this lane's first entry, owner block 0
-    int next_x, next_pos;                                      // chunk that is looked up next: distance of its entry 0, ring position
+    int chunk;                                                 // the 64 entries that are stored next: those of tile `chunk`
     int bucket;
-    float value;
+    unsigned short looked_up;
     int tile_lo, above_from, below_to;                         // lowest distance of the tile in hand; where the far sides begin
     bool near_tile;
     float cb_base, cb_above, cb_below, cb_tile;
@@ -101,9 +101,12 @@ struct Mods {
         t = t < -x.reach ? -x.reach : (t > x.reach ? x.reach : t);
         return x.buckets[t + x.reach];
     }
-    __device__ __forceinline__ float value_of(const int b, const int d) const {
+    __device__ __forceinline__ unsigned short entry(const int b) const {
         const int c = b < 0 ? 0 : (b >= x.num_buckets ? x.num_buckets - 1 : b);
-        const float v = (float)x.table[(size_t)c * p.H + h] * -1.4426950408889634f;
+        return reinterpret_cast<const unsigned short *>(x.table)[(size_t)c * p.H + h];
+    }
+    __device__ __forceinline__ float value_of(const unsigned short entry, const int d) const {
+        const float v = __builtin_bit_cast(float, (unsigned)entry << 16) * -1.4426950408889634f;
         return d > -n && d < ns ? v : 0.f;
     }
 
@@ -117,22 +120,22 @@ struct Mods {
             s = s < -(1 << 29) ? -(1 << 29) : (s > (1 << 29) ? (1 << 29) : s);
             start_pos = __builtin_amdgcn_readfirstlane(s);
             at = 4u * (unsigned)((BM - 32 * QB * wave - c + 4 * g) & (RING - 1));
-            next_x = -m0;
-            next_pos = BM & (RING - 1);
-            bucket = bucket_at(next_x + lane);
-            // the far sides: where their bias is a factor that fp32 holds with room on both sides (-inf is a mask, and goes through the ring)
-            auto far_cb = [&](const int b) {
-                const int i = b < 0 ? 0 : (b >= x.num_buckets ? x.num_buckets - 1 : b);
-                const float f = cb * __builtin_amdgcn_exp2f((float)x.table[(size_t)i * p.H + h] * -1.4426950408889634f);
-                return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
-            };
-            cb_base = cb;
-            cb_above = far_cb(x.buckets[2 * x.reach]);
-            cb_below = far_cb(x.buckets[0]);
-            above_from = cb_above > 0x1p-100f && cb_above < 0x1p100f ? x.reach : 0x7FFFFFFF;
-            below_to = cb_below > 0x1p-100f && cb_below < 0x1p100f ? -x.reach : (int)0x80000000;
-            const int first_row = m0 + 32 * QB * wave;
-            tile_lo = MODE == DKDV ? first_row - 63 - start_pos + 64 : -first_row - (32 * QB - 1) - start_pos - 64;
+            chunk = 2;
+            bucket = bucket_at(64 * own_chunk() - m0 + lane);
+            if constexpr (MODE == FWD) {
+                // the far sides: where their bias is a factor that fp32 holds with room on both sides (-inf is a mask, and goes through the ring)
+                auto far_cb = [&](const int b) {
+                    const int i = b < 0 ? 0 : (b >= x.num_buckets ? x.num_buckets - 1 : b);
+                    const float f = cb * __builtin_amdgcn_exp2f((float)x.table[(size_t)i * p.H + h] * -1.4426950408889634f);
+                    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
+                };
+                cb_base = cb;
+                cb_above = far_cb(x.buckets[2 * x.reach]);
+                cb_below = far_cb(x.buckets[0]);
+                above_from = cb_above > 0x1p-100f && cb_above < 0x1p100f ? x.reach : 0x7FFFFFFF;
+                below_to = cb_below > 0x1p-100f && cb_below < 0x1p100f ? -x.reach : (int)0x80000000;
+                tile_lo = -(m0 + 32 * QB * wave) - (32 * QB - 1) - start_pos - 64;
+            }
         }
         if constexpr (DROP) {
             keep = __builtin_amdgcn_readfirstlane(x.keep);
@@ -157,9 +160,9 @@ struct Mods {
             below = 0.f;
         }
     }
-    // Goes on to the next tile; whether its scores start from the ring.
+    // Forward: goes on to the next tile; whether its scores start from the ring.
     __device__ __forceinline__ bool next_tile() {
-        tile_lo += MODE == DKDV ? -64 : 64;
+        tile_lo += 64;
         const bool above = tile_lo >= above_from, below = tile_lo + 32 * QB + 62 <= below_to;
         const float a = cb_above, b = cb_below, c = cb_base;    // values: a choice between members would keep them all in memory
         cb_tile = above ? a : (below ? b : c);
@@ -169,33 +172,40 @@ struct Mods {
     __device__ __forceinline__ bool near() const { return near_tile; }
     __device__ __forceinline__ float cb_of_tile() const { return cb_tile; }
 
+    // The waves take turns with the entries of a tile: this wave's first one.
+    __device__ __forceinline__ int own_chunk() const { return 2 + ((wave - 2) & (NW - 1)); }
     // The entries of the first two tiles and of the owner tile in front of them.
     __device__ __forceinline__ void fill() {
         for (int e = threadIdx.x; e < BM + 128; e += THREADS) {
             const int d = e - BM - m0;
-            const float v = value_of(bucket_at(d), d);
+            const float v = value_of(entry(bucket_at(d)), d);
             ring[e] = v;
             if (e < MIRROR) ring[RING + e] = v;
         }
+        looked_up = entry(bucket);
+        bucket = bucket_at(64 * (own_chunk() + NW) - m0 + lane);
     }
-    // With a tile's loads: the values of its 64 entries, and the buckets of the next one's.  (Every wave does the same.)
-    __device__ __forceinline__ void request() {
-        value = value_of(bucket, next_x + lane);
-        next_x += 64;
-        bucket = bucket_at(next_x + lane);
-    }
-    // With a tile's stores.  The first two tiles are in the ring already.
+    // With a tile's stores: its entries, if it is this wave's turn, and the look-ups for the next turns: the table's entry for the
+    // next one, the bucket for the one behind it.  Nothing waits for them until then.  (With look-ups by all waves in
+    // every tile, a tile of the forward pass had 30 of 254 vector instructions more.)
     __device__ __forceinline__ void store() {
-        const int pos = (next_pos + 128) & (RING - 1);
-        ring[pos + lane] = value;
-        if (pos == 0 && lane < MIRROR) ring[RING + lane] = value;
-        next_pos = (next_pos + 64) & (RING - 1);
+        if ((chunk & (NW - 1)) == wave) {                      // uniform
+            const int pos = (BM + 64 * chunk) & (RING - 1), d = 64 * chunk - m0 + lane;
+            const float v = value_of(looked_up, d);
+            ring[pos + lane] = v;
+            if (pos == 0 && lane < MIRROR) ring[RING + lane] = v;
+            looked_up = entry(bucket);
+            bucket = bucket_at(d + 128 * NW);
+        }
+        ++chunk;
     }
     // What the score tile of owner block qb starts from, next streamed block.
     template <int qb>
     __device__ __forceinline__ void start(f32x16 &s) const {
-        const unsigned from = (at - 128u * qb) & (4 * RING - 1);
-        const float *const r = reinterpret_cast<const float *>(reinterpret_cast<const char *>(ring) + from);
+        // the address as one register: the offsets of all reads then fit their instructions
+        unsigned from = (unsigned)(uintptr_t)SIGATTN_LDS_PTR(float, ring) + ((at - 128u * qb) & (4 * RING - 1));
+        asm("" : "+v"(from));
+        const auto *const r = (const __attribute__((address_space(3))) float *)(uintptr_t)from;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = r[8 * (i / 4) + i % 4];
     }
@@ -396,15 +406,10 @@ struct Mods {
         sum_block(put, get, d0);
         sum_block(put, get, d1);
     }
-    // The unit of the sums, 1 / cb, changes by `f`.  (Near blocks lie in tiles of the same unit.)
-    __device__ __forceinline__ void rescale(const float f) {
-        if (!open_window) acc[0] *= f;
-    }
     // Behind the last block: what is left in the window, and the far sums (row 0 of the accumulators, lanes 0 to 15).
-    __device__ __forceinline__ void close(const float unit) {
+    __device__ __forceinline__ void close() {
         if (!active) return;
         if (open_window) { flush(); acc = f32x4{0.f, 0.f, 0.f, 0.f}; }
-        acc[0] *= unit;
         const bool all_below = k <= first;                     // not one block was near, or beyond
         float v = lane < 16 ? acc[0] : 0.f, u = lane < 16 ? below : 0.f;
 #pragma unroll

@@ -215,7 +215,8 @@ int forward(const void *q, const void *k, const void *v, void *o, const int32_t 
         const bool parts = need > 0 && workspace && workspace_bytes >= need && aligned16(workspace);
         return few::launch(few::Few{p, x, parts ? few_splits(B, L_k, H) : 1, few_groups(L_q), static_cast<float *>(workspace)}, d, s);
     }
-    return rel && drop ? mod::fwd_rel_dropout(p, x, d, s) : rel ? mod::fwd_rel(p, x, d, s) : mod::fwd_dropout(p, x, d, s);
+    if (d == 64) return rel && drop ? mod::fwd_rel_dropout_64(p, x, s) : rel ? mod::fwd_rel_64(p, x, s) : mod::fwd_dropout_64(p, x, s);
+    return rel && drop ? mod::fwd_rel_dropout_128(p, x, s) : rel ? mod::fwd_rel_128(p, x, s) : mod::fwd_dropout_128(p, x, s);
 }
 
 // The workspace of a backward call with a bias table: a row of sums for every 32 queries, and their sums by group.
@@ -256,7 +257,7 @@ int backward(const void *q, const void *k, const void *v, const void *d_o, void 
     pq.out0 = static_cast<bf16_t *>(dq);
     Extra x = extra(rel, drop);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (!rel) return mod::bwd_dropout(pk, pq, x, d, s);
+    if (!rel) return d == 64 ? mod::bwd_dropout_64(pk, pq, x, s) : mod::bwd_dropout_128(pk, pq, x, s);
 
     const int entries = RowSums::entries(rel->reach, L_q, L_k), groups = rel->q_start || B < 16 ? B : 16;
     const long long row_wgs = (long long)groups * H * (entries / 32 + 1), table_wgs = (long long)H * ((rel->num_buckets + TABLE_BUCKETS - 1) / TABLE_BUCKETS);
@@ -265,7 +266,9 @@ int backward(const void *q, const void *k, const void *v, const void *d_o, void 
     if (row_wgs > 2147483647LL || table_wgs > 2147483647LL) return SIGATTN_ERR_TOO_LARGE;
     x.part = static_cast<float *>(workspace);
     x.by_distance = x.part + row_floats(B, L_q, L_k, H, rel->reach);
-    if (int e = drop ? mod::bwd_rel_dropout(pk, pq, x, d, s) : mod::bwd_rel(pk, pq, x, d, s)) return e;
+    const int e64 = d != 64 ? 0 : drop ? mod::bwd_rel_dropout_64(pk, pq, x, s) : mod::bwd_rel_64(pk, pq, x, s);
+    const int e128 = d == 64 ? 0 : drop ? mod::bwd_rel_dropout_128(pk, pq, x, s) : mod::bwd_rel_128(pk, pq, x, s);
+    if (e64 || e128) return e64 ? e64 : e128;
     const Lengths l{seqlens_q, seqlens_k, rel->q_start, bias, L_q, L_k, H, B};
     if ((long long)B * ((L_q + 31) / 32) <= DIRECT_ROWS) return enqueue(sigattn_rel_table<true>, table_wgs, 256, 0, s, l, x, B, static_cast<bf16_t *>(dtable));
     if (int e = enqueue(sigattn_rel_rows, row_wgs, 256, 0, s, l, x, groups, seqs)) return e;

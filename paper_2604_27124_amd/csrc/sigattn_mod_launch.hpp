@@ -73,35 +73,41 @@ int launch_joint(Params kv, Params q, const Extra &x, hipStream_t stream) {
 // leaves the generator its registers.
 inline long long tiles128(const Params &p) { return ((long long)p.N + 127) / 128 * p.B * p.H; }
 
-template <bool BIAS, bool DROP>
-int launch_fwd(const Params &p, const Extra &x, int d, hipStream_t stream) {
-    if (d == 64) {
+template <int D, bool BIAS, bool DROP>
+int launch_fwd(const Params &p, const Extra &x, hipStream_t stream) {
+    if constexpr (D == 64) {
         if (p.N <= 128 || (long long)p.B * p.H * ((p.N + 255) / 256) <= 256) return launch_pass<FWD, 64, 1, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
         return launch_pass<FWD, 64, 2, 4, 72, 72, 2, 4, BIAS, DROP>(p, x, stream);
+    } else {
+        if (tiles128(p) <= 256) return launch_pass<FWD, 128, 1, 4, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
+        return launch_pass<FWD, 128, 1, 8, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
     }
-    if (tiles128(p) <= 256) return launch_pass<FWD, 128, 1, 4, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
-    return launch_pass<FWD, 128, 1, 8, 136, 144, 1, 4, BIAS, DROP>(p, x, stream);
 }
 
-template <bool BIAS, bool DROP>
-int launch_bwd(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream) {
-    if (d == 64) return launch_joint<64, 4, 72, 72, 2, 4, 4, BIAS, DROP>(kv, q, x, stream);
-    // with a bias the dQ pass spills 23 registers a tile in eight waves of 256 (backward of B = 8, H = 16, N = 2048 1308 us, so TODO)
-    if (BIAS || tiles128(kv) + tiles128(q) <= 512) return launch_joint<128, 4, 144, 136, 1, 4, 4, BIAS, DROP>(kv, q, x, stream);
-    if constexpr (!BIAS) {
+template <int D, bool BIAS, bool DROP>
+int launch_bwd(const Params &kv, const Params &q, const Extra &x, hipStream_t stream) {
+    if constexpr (D == 64) {
+        return launch_joint<64, 4, 72, 72, 2, 4, 4, BIAS, DROP>(kv, q, x, stream);
+    } else {
+        if (tiles128(kv) + tiles128(q) <= 512 || (BIAS && tiles128(q) <= 256)) return launch_joint<128, 4, 144, 136, 1, 4, 4, BIAS, DROP>(kv, q, x, stream);
         if (const int e = launch_pass<DKDV, 128, 1, 4, 144, 144, 1, 4, BIAS, DROP>(kv, x, stream)) return e;
         return launch_pass<DQ, 128, 1, 8, 144, 136, 1, 4, BIAS, DROP>(q, x, stream);
     }
-    return SIGATTN_ERR_LAUNCH;                                 // not reached
 }
 
-// defined in sigattn_rel.hip, sigattn_dropout.hip, sigattn_rel_dropout.hip
-int fwd_rel(const Params &p, const Extra &x, int d, hipStream_t stream);
-int bwd_rel(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream);
-int fwd_dropout(const Params &p, const Extra &x, int d, hipStream_t stream);
-int bwd_dropout(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream);
-int fwd_rel_dropout(const Params &p, const Extra &x, int d, hipStream_t stream);
-int bwd_rel_dropout(const Params &kv, const Params &q, const Extra &x, int d, hipStream_t stream);
+// A translation unit for each, so that they are compiled side by side: sigattn_{rel,dropout,rel_dropout}_{64,128}.hip.
+int fwd_rel_64(const Params &, const Extra &, hipStream_t);
+int fwd_rel_128(const Params &, const Extra &, hipStream_t);
+int fwd_dropout_64(const Params &, const Extra &, hipStream_t);
+int fwd_dropout_128(const Params &, const Extra &, hipStream_t);
+int fwd_rel_dropout_64(const Params &, const Extra &, hipStream_t);
+int fwd_rel_dropout_128(const Params &, const Extra &, hipStream_t);
+int bwd_rel_64(const Params &kv, const Params &q, const Extra &, hipStream_t);
+int bwd_rel_128(const Params &kv, const Params &q, const Extra &, hipStream_t);
+int bwd_dropout_64(const Params &kv, const Params &q, const Extra &, hipStream_t);
+int bwd_dropout_128(const Params &kv, const Params &q, const Extra &, hipStream_t);
+int bwd_rel_dropout_64(const Params &kv, const Params &q, const Extra &, hipStream_t);
+int bwd_rel_dropout_128(const Params &kv, const Params &q, const Extra &, hipStream_t);
 
 }  // namespace mod
 }  // namespace sigattn

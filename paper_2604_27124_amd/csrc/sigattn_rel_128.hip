@@ -1,0 +1,11 @@
+// Kernels with the relative position bias, d = 128: see sigattn_mod.hpp.
+#include "sigattn_mod_launch.hpp"
+
+namespace sigattn {
+namespace mod {
+
+int fwd_rel_128(const Params &p, const Extra &x, hipStream_t stream) { return launch_fwd<128, true, false>(p, x, stream); }
+int bwd_rel_128(const Params &kv, const Params &q, const Extra &x, hipStream_t stream) { return launch_bwd<128, true, false>(kv, q, x, stream); }
+
+}  // namespace mod
+}  // namespace sigattn
