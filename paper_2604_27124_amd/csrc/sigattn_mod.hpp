@@ -334,14 +334,16 @@ struct Mods {
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] = moved<ROW_SHL_8>(acc[i]);
     }
-    __device__ __forceinline__ void sum_block(unsigned char *const put, const unsigned char *const get, const u32x4 (&ds)[2]) {
+    __device__ __forceinline__ void sum_block(unsigned char *const put, const unsigned char *const get, const u32x4 (&ds)[2], const bool mine) {
         if (k >= first && k <= last) {                         // uniform
             if (!open_window) { below = acc[0]; acc = f32x4{0.f, 0.f, 0.f, 0.f}; open_window = true; }
+            if (mine) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {                      // rows 8 q + 4 g + 0..3
-                unsigned *const w = reinterpret_cast<unsigned *>(put) + 4 * q;
-                w[0] = ds[q / 2][2 * (q % 2)];
-                w[1] = ds[q / 2][2 * (q % 2) + 1];
+                for (int q = 0; q < 4; ++q) {                  // rows 8 q + 4 g + 0..3
+                    unsigned *const w = reinterpret_cast<unsigned *>(put) + 4 * q;
+                    w[0] = ds[q / 2][2 * (q % 2)];
+                    w[1] = ds[q / 2][2 * (q % 2) + 1];
+                }
             }
             asm volatile("" ::: "memory");
             float t[4] = {0.f, 0.f, 0.f, 0.f};
@@ -372,8 +374,17 @@ struct Mods {
             bf16x8 ones;
 #pragma unroll
             for (int i = 0; i < 8; ++i) ones[i] = (bf16_t)1.0f;
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[0]), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, ds[1]), acc, 0, 0, 0);
+            u32x4 d0 = ds[0], d1 = ds[1];
+            if (n - m0 - 32 * wave < 32) {                     // uniform
+                const unsigned ok = mine ? ~0u : 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    d0[i] &= ok;
+                    d1[i] &= ok;
+                }
+            }
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, d0), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, d1), acc, 0, 0, 0);
         }
         ++k;
     }
@@ -382,15 +393,6 @@ struct Mods {
                                         const u32x4 (&second_ds)[2]) {
         if (!active) return;                                   // uniform
         const int c = lane & 31, g = lane >> 5;
-        u32x4 d0[2] = {first_ds[0], first_ds[1]}, d1[2] = {second_ds[0], second_ds[1]};
-        if (n - m0 - 32 * wave < 32) {                         // rows behind the valid queries: a key of Inf would make them NaN
-            const unsigned ok = m0 + 32 * wave + c < n ? ~0u : 0u;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                d0[i / 4][i % 4] &= ok;
-                d1[i / 4][i % 4] &= ok;
-            }
-        }
         asm volatile("" ::: "memory");
         if (k <= last && k + 1 >= first) {
             const u32x4 z4 = {0u, 0u, 0u, 0u};
@@ -403,8 +405,9 @@ struct Mods {
         auto piece = [&](const int i) { return (i & 2 ? b : a) + (i & 1 ? (i & 2 ? b_step : a_step) : 0); };
         unsigned char *const put = piece(c & 3) + (c >> 2) * 128 + 4 * (15 - (c >> 1)) + 8 * g;
         const unsigned char *const get = piece(lane >> 4) + 8 * (lane & 15);
-        sum_block(put, get, d0);
-        sum_block(put, get, d1);
+        const bool mine = m0 + 32 * wave + c < n;              // rows behind the valid queries: a key of Inf would make them NaN
+        sum_block(put, get, first_ds, mine);
+        sum_block(put, get, second_ds, mine);
     }
     // Behind the last block: what is left in the window, and the far sums (row 0 of the accumulators, lanes 0 to 15).
     __device__ __forceinline__ void close() {

@@ -91,7 +91,7 @@ int launch_bwd(const Params &kv, const Params &q, const Extra &x, hipStream_t st
     } else {
         if (tiles128(kv) + tiles128(q) <= 512 || (BIAS && tiles128(q) <= 256)) return launch_joint<128, 4, 144, 136, 1, 4, 4, BIAS, DROP>(kv, q, x, stream);
         if (const int e = launch_pass<DKDV, 128, 1, 4, 144, 144, 1, 4, BIAS, DROP>(kv, x, stream)) return e;
-        return launch_pass<DQ, 128, 1, 8, 144, 136, 1, 4, BIAS, DROP>(q, x, stream);
+        return launch_pass<DQ, 128, 1, 8, 144, 136, 1, BIAS ? 2 : 4, BIAS, DROP>(q, x, stream);
     }
 }
 
