@@ -137,3 +137,240 @@ SMALL = [
 def test_parity(shape, op, d):
     B, Lq, Lk, H, nq, nk, reach, num, start = shape
     check(Case(B, Lq, Lk, H, d, nq, nk, op, reach, num, start, seed=d + len(op)))
+
+
+def same_bits(a, b):
+    return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("Lq", [3, 90])
+@pytest.mark.parametrize("low", [float("-inf"), -3.3895313892515355e38])
+def test_an_entry_of_minus_infinity_masks_its_pairs(Lq, low):
+    # all distances but 0..2 are masked; the queries from 40 on see no key at all
+    c = Case(2, Lq, 40, 2, 64, (Lq, Lq - 1), (40, 33), "rel", 5, 11, None, seed=3)
+    c.table[:] = low
+    c.table[5:8] = 0.25
+    ref = c.reference(table=np.where(c.table < -1e30, -np.inf, c.table).astype(np.float64))
+    assert Lq < 40 or np.all(ref[0][:, 41:] == 0)
+    check(c, ref)
+    if Lq > 16:
+        dtable = to_host(c.bwd()[3])
+        masked = np.ones(len(c.table), bool)
+        masked[5:8] = False
+        assert np.all(dtable[masked] == 0) and np.all(to_host(c.fwd())[:, 42:] == 0)
+
+
+@pytest.mark.parametrize("op,d,Lq", [("rel", 64, 70), ("both", 64, 70), ("rel", 128, 70), ("rel", 64, 5)])
+def test_what_only_padding_reaches_has_no_influence(op, d, Lq):
+    # NaN and Inf in padded rows, NaN in table entries of distances that no valid pair has
+    c = Case(2, Lq, 130, 2, d, (min(Lq, 41), 3), (77, 50), op, 129, 259, None, seed=9).upload()
+    want = [t.clone() for t in (c.fwd(), *c.bwd())]
+    t = c.t
+    for n, (lens, names) in enumerate(((c.nq, ("q", "g")), (c.nk, ("k", "v")))):
+        for name in names:
+            for z in range(2):
+                t[name][z, int(lens[z]):] = float("nan") if z else float("inf")
+    t["table"][:129 - 40] = float("nan")                                   # distances below -40
+    t["table"][129 + 77:] = float("nan")                                   # and above 76
+    for a, b in zip((c.fwd(), *c.bwd()), want):
+        assert same_bits(a, b)
+    # a NaN that valid pairs do reach shows
+    t["table"][129] = float("nan")
+    assert bool(torch.isnan(c.fwd()).any())
+
+
+def test_an_infinite_key_leaves_the_table_gradient_finite():
+    # P is 0 or 1 against it and dS 0; padded queries of its tile have scores 0 x Inf
+    c = Case(1, 50, 64, 1, 64, (37,), (64,), "rel", 7, 15, None, seed=5)
+    c.k[0, 20, 0, 3] = np.inf
+    with np.errstate(invalid="ignore"):
+        ref = c.reference()
+        squares = c.ds_squares()
+    c.upload()
+    dtable = to_host(c.bwd()[3])
+    assert np.all(np.isfinite(ref[4])) and np.all(np.abs(dtable - ref[4]) <= BWD_TOL * (np.abs(ref[4]) + np.sqrt(squares)))
+
+
+def test_buckets_out_of_range_are_clamped():
+    c = Case(1, 60, 60, 2, 64, (60,), (60,), "rel", 3, 4, None, seed=6)
+    c.buckets[:] = (-7, 0, 1, 99, 2, 3, 2 ** 31 - 1)
+    check(c)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_table_of_zeros_gives_the_plain_call(d):
+    c = Case(3, 300, 200, 2, d, (300, 129, 0), (200, 77, 150), "rel", 40, 8, None, seed=7, table_std=0.0).upload()
+    t = c.t
+    common = (t["nq"], t["nk"], t["bias"], c.scale)
+    assert same_bits(c.fwd(), A.sigmoid_attn_cross_fwd(t["q"], t["k"], t["v"], *common))
+    for a, b in zip(c.bwd()[:3], A.sigmoid_attn_cross_bwd(t["q"], t["k"], t["v"], t["g"], *common)):
+        assert same_bits(a, b)
+
+
+@pytest.mark.parametrize("op", ["dropout", "both"])
+def test_no_dropout_and_nearly_all(op):
+    c = Case(2, 90, 70, 2, 64, (90, 33), (70, 64), op, 9, 8, None, p=0.0, seed=8).upload()
+    t = c.t
+    common = (t["nq"], t["nk"], t["bias"], c.scale)
+    plain = A.sigmoid_attn_cross_fwd(t["q"], t["k"], t["v"], *common) if op == "dropout" else \
+        A.sigmoid_attn_rel_fwd(t["q"], t["k"], t["v"], *common, t["table"], t["buckets"])
+    assert same_bits(c.fwd(), plain)
+    c.p = 1e-6                                                             # rounds to none
+    assert same_bits(c.fwd(), plain)
+    check(Case(1, 130, 130, 1, 64, (130,), (130,), op, 9, 8, None, p=0.97, seed=8))
+    c.p = 1.0 - 2.0 ** -24                                                 # one weight of 65536 stays at least: finite
+    assert bool(torch.isfinite(c.fwd()).all())
+
+
+def test_seed_and_offset():
+    c = Case(1, 64, 96, 2, 64, (64,), (96,), "dropout", seed=10, rng=(-5, 2 ** 40 + 3)).upload()
+    check(c)
+    base = c.fwd()
+    c.t["rng"].copy_(torch.tensor([-5, 3]))                                # the offset counts modulo 2^32
+    assert same_bits(c.fwd(), base)
+    for other in ((-5, 4), (-6, 3), (-5 + 2 ** 32, 3)):
+        c.t["rng"].copy_(torch.tensor(other))
+        assert not same_bits(c.fwd(), base)
+
+
+def test_share_of_weights_that_stay():
+    # V of ones and P of one half everywhere: O counts what stays
+    B, N, H, d, p = 2, 1024, 3, 64, 0.1
+    z = torch.zeros(B, N, H, d, dtype=torch.bfloat16, device="cuda")
+    n, b = torch.full((B,), N, dtype=torch.int32, device="cuda"), torch.zeros(B, device="cuda")
+    o = A.sigmoid_attn_dropout_fwd(z, z, torch.ones_like(z), n, n, b, 1.0, p, torch.tensor([7, 0], device="cuda"))[..., 0].double()
+    keep = M.kept(p) / 65536
+    # mean of N^2 H B decisions, and 2^-9 for the rounding of each O, which has no preferred direction (six deviations of either)
+    assert abs(float(o.mean()) * keep * 2 / N - keep) < 6 * np.sqrt(keep * (1 - keep) / (B * H * N * N)) + 6 * 2.0 ** -9 / np.sqrt(B * H * N)
+
+
+@pytest.mark.parametrize("op", ["rel", "dropout", "both"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_sequence_does_not_depend_on_its_batch(op, d):
+    # bias, alone in the batch and among others: the same bits (with dropout the mask goes by the place in the batch)
+    c = Case(3, 300, 300, 2, d, (300, 200, 131), (300, 200, 131), op, 40, 16, None, seed=12).upload()
+    one = Case(1, 300, 300, 2, d, (300,), (300,), op, 40, 16, None, seed=12)
+    one.__dict__.update({n: getattr(c, n)[:1] for n in ("q", "k", "v", "g", "nq", "nk", "bias")}, table=c.table, buckets=c.buckets)
+    one.upload()
+    for a, b in zip((c.fwd(), *c.bwd()[:3]), (one.fwd(), *one.bwd()[:3])):
+        assert same_bits(a[:1], b)
+
+
+@pytest.mark.parametrize("op", ["rel", "dropout", "both"])
+@pytest.mark.parametrize("Lq", [2, 100])
+def test_other_streams_and_the_python_way(op, Lq):
+    c = Case(2, Lq, 3000, 2, 64, (Lq, 1), (3000, 2048), op, 100, 32, (2900, 0), seed=13).upload()
+    want = (c.fwd(), *c.bwd())                                             # native calls
+    here = torch.cuda.current_stream()
+    for a, b in zip((c.fwd(stream=here), *c.bwd(stream=here)), want):      # marshalled in Python
+        assert same_bits(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(here)
+    outs = [poisoned(x) for x in want]
+    names = ("dq", "dk", "dv", "dtable")
+    c.fwd(out=outs[0], stream=side)
+    c.bwd(**dict(zip(names, outs[1:])), stream=side)
+    with torch.cuda.stream(side):
+        again = (c.fwd(), *c.bwd())
+    torch.cuda.synchronize()
+    for got in (outs, again):
+        for a, b in zip(got, want):
+            assert same_bits(a, b)
+
+
+def test_few_queries_with_and_without_a_workspace():
+    c = Case(1, 7, 5000, 2, 64, (7,), (4900,), "rel", 100, 32, (4893,), seed=14).upload()
+    need = A.sigmoid_attn_rel_fwd_workspace_bytes(1, 7, 5000, 2, 64)
+    assert need > 0 and A.sigmoid_attn_rel_fwd_workspace_bytes(64, 7, 5000, 12, 64) == 0
+    split, whole = c.fwd(workspace=torch.empty(need, dtype=torch.uint8, device="cuda")), c.fwd(workspace=torch.empty(0, device="cuda"))
+    assert same_bits(split, c.fwd())
+    ref = c.reference()[0]
+    for o in (split, whole):
+        # fp32 throughout: half a bf16 step of the value, and sums of 4900 fp32 terms
+        assert np.all(np.abs(to_host(o) - ref) <= 2.0 ** -8 * np.abs(ref) + 1e-5 * np.abs(ref).max())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_step_in_a_hip_graph(d):
+    """Bias and dropout captured and replayed, with another offset each time; the workspace and outputs are the program's."""
+    c = Case(2, 300, 260, 2, d, (300, 131), (260, 77), "both", 60, 32, None, seed=15).upload()
+    t = c.t
+    ws = torch.empty(A.sigmoid_attn_rel_bwd_workspace_bytes(2, 300, 260, 2, d, 60), dtype=torch.uint8, device="cuda")
+    outs = dict(dq=poisoned(t["q"]), dk=poisoned(t["k"]), dv=poisoned(t["v"]), dtable=poisoned(t["table"]))
+    o = poisoned(t["q"])
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.fwd(out=o), c.bwd(**outs, workspace=ws)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            c.fwd(out=o), c.bwd(**outs, workspace=ws)
+    torch.cuda.synchronize()
+    for replay in range(4):
+        t["rng"][1] = 100 + replay
+        for x in (o, *outs.values()):
+            x.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((o, *outs.values()), (c.fwd(), *c.bwd())):
+            assert same_bits(a, b), replay
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own():
+    a, b = (Case(2, 400, 400, 2, 64, (400, 300), (400, 300), "both", 50, 16, None, seed=s).upload() for s in (16, 17))
+    want = [(x.fwd(), *x.bwd()) for x in (a, b)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for x, s in zip((a, b), streams):
+        with torch.cuda.stream(s):
+            got.append((x.fwd(), *x.bwd()))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for x, y in zip(g, w):
+            assert same_bits(x, y)
+
+
+@pytest.mark.parametrize("Lq", [1, 20])
+def test_offsets_beyond_32_bits(Lq):
+    """A context of 4.5 GB a tensor: the last rows lie behind 2^32 bytes."""
+    H, d, Lk = 16, 128, 1100000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.empty(1, Lk, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(2))
+    q = torch.empty(1, Lq, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    table = torch.empty(8, H, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    buckets, start = A.sigmoid_attn_rel_buckets(8, 30).cuda(), torch.tensor([Lk - Lq], dtype=torch.int32, device="cuda")
+    nq, nk = torch.tensor([Lq], dtype=torch.int32, device="cuda"), torch.tensor([Lk], dtype=torch.int32, device="cuda")
+    bias, scale = torch.tensor([-8.0], device="cuda"), d ** -0.5
+    o = A.sigmoid_attn_rel_fwd(q, k, v, nq, nk, bias, scale, table, buckets, q_start=start)
+    away = torch.arange(Lk, device="cuda")[None] - torch.arange(Lq, device="cuda")[:, None] - (Lk - Lq)
+    which = buckets.long()[away.clamp(-30, 30) + 30]
+    for h in (0, H - 1):
+        x = scale * (q[0, :, h].double() @ k[0, :, h].double().t().contiguous()) - 8.0 + table[:, h].double()[which]
+        ref = torch.sigmoid(x) @ v[0, :, h].double()
+        assert float((o[0, :, h].double() - ref).abs().max() / ref.abs().max()) < FWD_TOL
+
+
+def test_refusals():
+    c = Case(2, 30, 40, 2, 64, (30, 3), (40, 4), seed=18).upload()
+    t, common = c.t, (c.t["nq"], c.t["nk"], c.t["bias"], c.scale)
+    q, k, v, g = t["q"], t["k"], t["v"], t["g"]
+    fine = dict(table=t["table"], buckets=t["buckets"])
+    for bad in (dict(table=t["table"].float()), dict(table=t["table"].t()), dict(table=t["table"][:, :1]), dict(buckets=t["buckets"][:-1]),
+                dict(buckets=t["buckets"].long()), dict(buckets=t["buckets"].cpu()), dict(q_start=t["nq"][:1]), dict(out=k), dict(out=q.float())):
+        with pytest.raises(ValueError):
+            A.sigmoid_attn_rel_fwd(q, k, v, *common, **{**fine, **bad})
+    for bad in (dict(dtable=t["table"].float()), dict(dq=k), dict(dk=q)):
+        with pytest.raises(ValueError):
+            A.sigmoid_attn_rel_bwd(q, k, v, g, *common, **{**fine, **bad})
+    with pytest.raises(A.SigAttnError) as e:
+        A.sigmoid_attn_rel_bwd(q, k, v, g, *common, **fine, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == A.SIGATTN_ERR_WORKSPACE
+    for p, rng in ((1.0, t["rng"]), (-0.1, t["rng"]), (float("nan"), t["rng"])):
+        with pytest.raises(A.SigAttnError):
+            A.sigmoid_attn_dropout_fwd(q, k, v, *common, p, rng)
+    for rng in (t["rng"].int(), t["rng"][:1], t["rng"].cpu()):
+        with pytest.raises(ValueError):
+            A.sigmoid_attn_dropout_fwd(q, k, v, *common, 0.1, rng)
+    with pytest.raises(ValueError):
+        A.sigmoid_attn_dropout_fwd(q.transpose(1, 2), k, v, *common, 0.1, t["rng"])

@@ -1,0 +1,92 @@
+"""Properties of the emitted gfx950 code of the kernels with a bias and with dropout that their synchronisation relies on: the same
+that test_isa_invariants.py checks for the plain ones.  Cross-compiled here, no GPU needed."""
+import os
+import re
+import subprocess
+from concurrent.futures import ThreadPoolExecutor
+
+import pytest
+
+from paper_2604_27124_amd import build as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+UNITS = ("sigattn_rel_dropout_64", "sigattn_rel_128", "sigattn_dropout_128")
+
+
+@pytest.fixture(scope="module")
+def kernels(tmp_path_factory):
+    """(unit, name) -> instruction lines and bytes of scratch of each attention kernel."""
+    out = tmp_path_factory.mktemp("isa")
+    flags = [f for f in B.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
+
+    def compile(unit):
+        subprocess.run([B.hipcc(), *flags, "-I", os.path.join(ROOT, "include"), "-S", "--cuda-device-only", "-o", str(out / unit),
+                        os.path.join(B.CSRC, unit + ".hip")], check=True, capture_output=True)
+
+    with ThreadPoolExecutor(len(UNITS)) as pool:
+        list(pool.map(compile, UNITS))
+    result = {}
+    for unit in UNITS:
+        name = None
+        for line in (out / unit).read_text().split("\n"):
+            m = re.match(r"^(_Z\w+):", line)
+            if m:
+                name = (unit, m.group(1)) if "sigattn_mod" in m.group(1) else None
+                if name:
+                    result[name] = {"body": [], "scratch": None}
+            elif name and re.match(r"^; ScratchSize: \d+", line):
+                result[name]["scratch"] = int(line.split()[-1])
+            elif name and result[name]["scratch"] is None:
+                ins = line.split(";")[0].strip()
+                if ins and not ins.startswith("."):
+                    result[name]["body"].append(ins)
+    return result
+
+
+def loops(name):
+    """Passes over the streamed tiles: two in a joint backward kernel; a forward kernel with a bias has a loop for each kind of tile."""
+    if "sigattn_mod_bwd" in name[1]:
+        return 2
+    return 2 if "sigattn_modILi0E" in name[1] and "rel" in name[0] else 1
+
+
+def test_every_kernel_is_looked_at(kernels):
+    assert sorted(u for u, _ in kernels) == ["sigattn_dropout_128"] * 5 + ["sigattn_rel_128"] * 5 + ["sigattn_rel_dropout_64"] * 3
+    assert all(k["scratch"] is not None and any(i.startswith("s_endpgm") for i in k["body"]) for k in kernels.values())
+
+
+def test_tile_barrier_counts_its_reads(kernels):
+    for name, k in kernels.items():
+        body, partial = k["body"], []
+        for i, ins in enumerate(body):
+            if ins != "s_barrier":
+                continue
+            w = i - 1
+            while re.match(r"(v_|s_)(?!waitcnt|load|buffer_load|barrier)", body[w]) and i - w < 8:
+                w -= 1
+            m = re.match(r"s_waitcnt (?:vmcnt\(\d+\) )?lgkmcnt\((\d+)\)$", body[w])
+            assert m, f"{name}: barrier without an LDS wait in front of it ({body[w]!r})"
+            if int(m.group(1)) == 0:
+                continue
+            assert w == i - 1, f"{name}: instructions between a partial LDS wait and its barrier"
+            reads, j = 0, i - 2
+            while j >= 0 and not body[j].startswith("ds_write"):
+                assert not body[j].startswith(("s_load", "s_buffer_load", "s_barrier")), f"{name}: {body[j]!r} between the tile store and its barrier"
+                reads += body[j].startswith("ds_")
+                j -= 1
+            # no fewer than may stay in flight: then all writes in front of them have completed
+            assert reads >= int(m.group(1)), f"{name}: lgkmcnt({m.group(1)}) but {reads} LDS operations follow the tile store"
+            partial.append(i)
+        assert len(partial) == 4 * loops(name), f"{name}: {len(partial)} tile barriers"
+
+
+def test_no_packed_fp32_and_few_spills(kernels):
+    for name, k in kernels.items():
+        assert not any(re.match(r"v_pk_(add|mul|fma)_f32", i) for i in k["body"]), name
+        # the eight-wave dQ pass of d = 128 with a bias parks some registers a tile; the four-wave dK/dV pass around its loop
+        assert k["scratch"] <= (128 if "Li128E" in name[1] else 0), f"{name}: {k['scratch']} bytes"
+
+
+def test_sums_by_distance_use_no_atomics(kernels):
+    for name, k in kernels.items():
+        assert not any("atomic" in i or re.match(r"ds_(add|pk_add)", i) for i in k["body"]), name
