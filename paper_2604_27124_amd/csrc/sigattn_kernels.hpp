@@ -1167,17 +1167,21 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         const auto d1 = __builtin_amdgcn_make_buffer_rsrc(uniform_ptr((MODE == DKDV ? p.out1 : p.out0) + base), 0, bytes, 0x00027000);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-            const bool ok = off + qb * block_bytes < valid;
+            // The block's offset belongs to the lanes' offset, not into the scalar one: behind a store with a scalar offset the compiler
+            // leaves no wait before its data registers are written again, and the store took the new values in some lanes (one
+            // element in 6000 of the forward pass with dropout, where the next instruction is a multiplication into the first register).
+            const int at = off + qb * block_bytes;
+            const bool ok = at < valid;
             const u32x4 z4 = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
                 for (int pr = 0; pr < 2; ++pr) {
                     const u32x4 w0 = chunk(acc0[qb][mb], pr, oscale);
-                    __builtin_amdgcn_raw_buffer_store_b128(ok ? w0 : z4, d0, off + 2 * TL_ACC0::out_col(mb, 2 * pr), qb * block_bytes, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(ok ? w0 : z4, d0, at + 2 * TL_ACC0::out_col(mb, 2 * pr), 0, 0);
                     if (MODE == DKDV) {
                         const u32x4 w1 = chunk(acc1[MODE == DKDV ? qb : 0][MODE == DKDV ? mb : 0], pr, used);
-                        __builtin_amdgcn_raw_buffer_store_b128(ok ? w1 : z4, d1, off + 2 * TL_ACC1::out_col(mb, 2 * pr), qb * block_bytes, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(ok ? w1 : z4, d1, at + 2 * TL_ACC1::out_col(mb, 2 * pr), 0, 0);
                     }
                 }
             }

@@ -115,3 +115,22 @@ def test_no_packed_fp32_and_few_spills(kernels):
 def test_no_floating_point_atomics(kernels):
     for name, k in kernels.items():            # (the work mapping counts tiles with integer ones)
         assert not any(re.match(r"(global|flat|buffer)_atomic|ds_(pk_)?add\w*_(f|bf)", i) for i in k["body"]), name
+
+
+def test_wide_stores_keep_their_data(kernels):
+    """A store of more than two dwords reads its data registers a little later than it is issued; with a scalar offset the compiler does not
+    count on that.  So no such store is followed at once by an instruction that writes them."""
+    def registers(operand):
+        m = re.match(r"v\[(\d+):(\d+)\]$|v(\d+)$", operand)
+        return set() if m is None else set(range(int(m.group(1)), int(m.group(2)) + 1)) if m.group(1) else {int(m.group(3))}
+
+    for name, k in kernels.items():
+        ins = [i for i in k["body"] if not i.endswith(":")]
+        for at, store in enumerate(ins):
+            m = re.match(r"buffer_store_dwordx[34] (\S+), .*, s\d+ offen", store)
+            if m is None:
+                continue
+            for after in ins[at + 1:at + 3]:
+                if after.startswith("s_nop"):
+                    break
+                assert not (after.startswith("v_") and registers(after.split()[1].rstrip(",")) & registers(m.group(1))), f"{name}: {store} / {after}"
