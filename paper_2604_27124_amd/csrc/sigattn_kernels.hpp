@@ -479,6 +479,7 @@ __device__ __forceinline__ bf16_t *uniform_ptr(const bf16_t *p) {
 
 // What run_pass() takes in where scores and weights are changed on their way (sigattn_mod.hpp has such types); this one changes nothing.
 struct Plain {
+    static constexpr bool SCALED = true;           // scale log2 e is folded into the owner rows of the scores, rounded to bf16
     static constexpr bool BIASED = false;          // score accumulators start from values of the type's own, not from zeros
     static constexpr bool SIFTED = false;          // weights of a finished block pass through the type before they are contracted
     static constexpr bool SUMMED = false;          // dS of a finished block is looked at (DQ)
@@ -566,7 +567,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     // operand), so t' leaves the MFMA ready for exp2; cb rides on the FMA that forms the denominator.
     // The exponent of cb is clamped to +-126 (|bias| <= 87.3 is exact; beyond that sigma is saturated).
     // cb is finite and non-zero, so cb 2^t' is 0, finite or +inf but never NaN, and P lands in [0, 1].
-    const float c1 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, -p.scale * LOG2E)));
+    float c1 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, -p.scale * LOG2E)));
+    if constexpr (!Mod::SCALED) c1 = mod.factor(c1);               // not folded in: multiplied with the finished score
     const float cb = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int,
         __builtin_amdgcn_exp2f(__builtin_fminf(__builtin_fmaxf(-p.bias[z] * LOG2E, -126.0f), 126.0f)))));
 
@@ -602,6 +604,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         __builtin_amdgcn_sched_barrier(0);
     };
     auto scale_owner = [&]() {
+        if constexpr (!Mod::SCALED) return;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -866,8 +869,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 };
                 constexpr IntC<0> A_{};
                 constexpr IntC<1> B_{};
-                if constexpr (o == 0) s[ra] = __builtin_amdgcn_exp2f(s[ra]);
-                else if constexpr (o == 1) s[rb] = __builtin_amdgcn_exp2f(s[rb]);
+                if constexpr (o == 0) s[ra] = __builtin_amdgcn_exp2f(Mod::SCALED ? s[ra] : s[ra] * c1);
+                else if constexpr (o == 1) s[rb] = __builtin_amdgcn_exp2f(Mod::SCALED ? s[rb] : s[rb] * c1);
                 else if constexpr (o == 2) set_y(A_, __builtin_fmaf(cb_now, s[ra], 1.0f));
                 else if constexpr (o == 3) set_y(B_, __builtin_fmaf(cb_now, s[rb], 1.0f));
                 else if constexpr (o == 4) set_y(A_, __builtin_amdgcn_rcpf(y_of(A_)));
@@ -895,7 +898,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     using F_ = IntC<0>;
 
     // ---- prologue: tiles 0 and 1 of the stream into the ring, tile 2 into registers
-    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0, cb);   // one owner tile a workgroup
+    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0, cb, c1);   // one owner tile a workgroup
     {   // the first three tiles are requested back to back, so their latencies overlap
         load_tile();
         u32x4 a1[C::PER], a2[C::PER];
