@@ -767,13 +767,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     // (a quarter of a tile earlier), which only the d = 128 forward pass gains from (12 x 1537 rows, H = 16: 172 -> 167 us;
     // d = 64, N = 8192, forward + backward 1543 -> 1559 us).
     constexpr bool LOAD_EARLY = MODE == FWD && D == 128;
-    // cb of the block whose sigmoid is made.  BIASED, forward: scores of a tile whose pairs all have one bias start from zeros, and the
-    // bias rides on cb like that of the sequence.
-    constexpr bool KINDS = Mod::BIASED && MODE == FWD;
-    using Near = IntC<Mod::BIASED ? 1 : 0>;
-    float cb_now = cb;
-    auto step = [&](auto has_prev_c, auto has_next_c, auto drain_c, auto nb_c, auto slot, auto store_at_c, const int store_slot, auto near_c) {
-        constexpr bool START = Mod::BIASED && decltype(near_c)::value;   // the next block's score tile starts from values in LDS
+    auto step = [&](auto has_prev_c, auto has_next_c, auto drain_c, auto nb_c, auto slot, auto store_at_c, const int store_slot) {
         constexpr int STORE_AT = decltype(store_at_c)::value;   // slot before which the staged tile goes to LDS (-1: never)
         constexpr bool HAS_PREV = decltype(has_prev_c)::value;  // a block went before: its output contractions
         constexpr bool HAS_NEXT = decltype(has_next_c)::value;  // a block follows: compute its scores
@@ -793,8 +787,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 if constexpr (!DRAIN) mod.template slot<k, SLOTS>();
             }
             if constexpr (Mod::BIASED) {
-                if constexpr (HAS_NEXT && !DRAIN && k == 0 && !START) mod.advance();
-                if constexpr (HAS_NEXT && !DRAIN && k == 0 && START) {
+                if constexpr (HAS_NEXT && !DRAIN && k == 0) {
                     static_for<0, QB>([&](auto q_) { mod.template start<decltype(q_)::value>(sbuf[PAR ^ 1][decltype(q_)::value]); });
                     mod.advance();
                 }
@@ -818,7 +811,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                     constexpr int ks = Order::ks(j), which = Order::which(j);
                     if constexpr (which == 0)
                         sbuf[PAR ^ 1][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            ring[(G0 + pos) % RING], xa[qb][ks], ks == 0 && !START ? zero : sbuf[PAR ^ 1][qb], 0, 0, 0);
+                            ring[(G0 + pos) % RING], xa[qb][ks], ks == 0 && !Mod::BIASED ? zero : sbuf[PAR ^ 1][qb], 0, 0, 0);
                     else
                         dbuf[PAR ^ 1][HAS2 ? qb : 0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                             ring[(G0 + pos) % RING], xb[HAS2 ? qb : 0][HAS2 ? ks : 0],
@@ -871,8 +864,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
                 constexpr IntC<1> B_{};
                 if constexpr (o == 0) s[ra] = __builtin_amdgcn_exp2f(Mod::SCALED ? s[ra] : s[ra] * c1);
                 else if constexpr (o == 1) s[rb] = __builtin_amdgcn_exp2f(Mod::SCALED ? s[rb] : s[rb] * c1);
-                else if constexpr (o == 2) set_y(A_, __builtin_fmaf(cb_now, s[ra], 1.0f));
-                else if constexpr (o == 3) set_y(B_, __builtin_fmaf(cb_now, s[rb], 1.0f));
+                else if constexpr (o == 2) set_y(A_, __builtin_fmaf(cb, s[ra], 1.0f));
+                else if constexpr (o == 3) set_y(B_, __builtin_fmaf(cb, s[rb], 1.0f));
                 else if constexpr (o == 4) set_y(A_, __builtin_amdgcn_rcpf(y_of(A_)));
                 else if constexpr (o == 5) set_y(B_, __builtin_amdgcn_rcpf(y_of(B_)));
                 else {
@@ -898,7 +891,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     using F_ = IntC<0>;
 
     // ---- prologue: tiles 0 and 1 of the stream into the ring, tile 2 into registers
-    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0, cb, c1);   // one owner tile a workgroup
+    if constexpr (Mod::BIASED || Mod::SIFTED || Mod::SUMMED) mod.open(z, h, n, ns, m0, c1);   // one owner tile a workgroup
     {   // the first three tiles are requested back to back, so their latencies overlap
         load_tile();
         u32x4 a1[C::PER], a2[C::PER];
@@ -969,19 +962,18 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto tile_body = [&](auto slot_c, auto near_c) {   // from the second block of a tile through the first of the next
+    auto tile_body = [&](auto slot_c) {            // from the second block of a tile through the first of the next
         constexpr int slot = decltype(slot_c)::value;
         finish(IntC<0>{});
         static_for<1, NB>([&](auto nb_) {
-            if constexpr (decltype(nb_)::value + 1 < NB) step(T_{}, T_{}, F_{}, nb_, slot_c, NoStore{}, 0, near_c);
-            else step(T_{}, T_{}, F_{}, nb_, slot_c, StoreAt{}, (slot + 2) & (C::NBUF - 1), near_c);
+            if constexpr (decltype(nb_)::value + 1 < NB) step(T_{}, T_{}, F_{}, nb_, slot_c, NoStore{}, 0);
+            else step(T_{}, T_{}, F_{}, nb_, slot_c, StoreAt{}, (slot + 2) & (C::NBUF - 1));
         });
         asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(READS_AFTER) : "memory");
         if constexpr (!LOAD_EARLY) load_tile();
         finish(IntC<1>{});
         sums(IntC<(slot + 3) & (C::NBUF - 1)>{});      // the tile before this one; stored next: two steps on
-        if constexpr (KINDS) cb_now = mod.cb_of_tile();
-        step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0, near_c);
+        step(T_{}, T_{}, F_{}, IntC<0>{}, IntC<(slot + 1) & (C::NBUF - 1)>{}, NoStore{}, 0);
     };
 
     // P and dS of the streamed rows behind the valid length, in block nb of the last tile: exact zeros, as packed for the
@@ -1029,13 +1021,7 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         {
             const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if constexpr (Mod::BIASED) {
-                bool near = true;
-                if constexpr (KINDS) near = mod.next_tile();
-                static_for<0, QB>([&](auto q_) {
-                    constexpr int qb = decltype(q_)::value;
-                    if (near) mod.template start<qb>(sbuf[0][qb]);
-                    else sbuf[0][qb] = zero;
-                });
+                static_for<0, QB>([&](auto q_) { mod.template start<decltype(q_)::value>(sbuf[0][decltype(q_)::value]); });
                 mod.advance();
             }
 #pragma unroll
@@ -1056,44 +1042,14 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         static_for<0, RING - 1>([&](auto J_) {
             if constexpr (Order::score(decltype(J_)::value)) ring[decltype(J_)::value % RING] = fetch(J_, DynInt{slot_rt}, IntC<0>{});
         });
-        if constexpr (KINDS) {
-            cb_now = mod.cb_of_tile();
-            if (mod.near()) step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, T_{});
-            else step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, F_{});
-        } else {
-            step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0, Near{});
-        }
+        step(F_{}, T_{}, F_{}, IntC<0>{}, DynInt{slot_rt}, NoStore{}, 0);
 
         int t = ntiles - 1;
-        if constexpr (KINDS) {
-            // Tiles of one kind follow each other (one far side, near, the other far side), so each kind has a loop of its own.
-            mod.next_tile();
-            auto run = [&](auto near_c) {
-                constexpr bool NEAR = decltype(near_c)::value;
-                auto go = [&](auto slot_c) {
-                    tile_body(slot_c, near_c);
-                    slot_rt = (decltype(slot_c)::value + 1) & (C::NBUF - 1);
-                    --t;
-                    mod.next_tile();
-                };
-                while (t > 0 && mod.near() == NEAR) {
-                    if (slot_rt == 0) go(IntC<0>{});
-                    if (t > 0 && mod.near() == NEAR && slot_rt == 1) go(IntC<1>{});
-                    if (t > 0 && mod.near() == NEAR && slot_rt == 2) go(IntC<2>{});
-                    if (t > 0 && mod.near() == NEAR && slot_rt == 3) go(IntC<3>{});
-                }
-            };
-            while (t > 0) {
-                run(F_{});
-                run(T_{});
-            }
-        } else {
-            while (t > 0) {
-                if (slot_rt == 0) { tile_body(IntC<0>{}, Near{}); slot_rt = 1; --t; }
-                if (t > 0 && slot_rt == 1) { tile_body(IntC<1>{}, Near{}); slot_rt = 2; --t; }
-                if (t > 0 && slot_rt == 2) { tile_body(IntC<2>{}, Near{}); slot_rt = 3; --t; }
-                if (t > 0 && slot_rt == 3) { tile_body(IntC<3>{}, Near{}); slot_rt = 0; --t; }
-            }
+        while (t > 0) {
+            if (slot_rt == 0) { tile_body(IntC<0>{}); slot_rt = 1; --t; }
+            if (t > 0 && slot_rt == 1) { tile_body(IntC<1>{}); slot_rt = 2; --t; }
+            if (t > 0 && slot_rt == 2) { tile_body(IntC<2>{}); slot_rt = 3; --t; }
+            if (t > 0 && slot_rt == 3) { tile_body(IntC<3>{}); slot_rt = 0; --t; }
         }
 
         // ---- last tile.  The owner rows are not needed any more: request those of the next owner tile.
@@ -1107,13 +1063,13 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             mask_block(IntC<0>{});
             finish(IntC<0>{});
             static_for<1, NB>([&](auto nb_) {
-                step(T_{}, IntC<(decltype(nb_)::value + 1 < NB) ? 1 : 0>{}, F_{}, nb_, slot, NoStore{}, 0, F_{});
+                step(T_{}, IntC<(decltype(nb_)::value + 1 < NB) ? 1 : 0>{}, F_{}, nb_, slot, NoStore{}, 0);
                 mask_block(nb_);
                 finish(nb_);
             });
             sums(DynInt{(slot_rt + 2) & (C::NBUF - 1)});   // no tile of its own: last read before the barrier behind the tile before
             const DynInt slot_next{(slot_rt + 1) & (C::NBUF - 1)};
-            step(T_{}, F_{}, T_{}, IntC<0>{}, slot_next, NoStore{}, 0, F_{});
+            step(T_{}, F_{}, T_{}, IntC<0>{}, slot_next, NoStore{}, 0);
             if (more) {
                 store_tile((slot_rt + 2) & (C::NBUF - 1));
                 load_tile();

@@ -9,9 +9,9 @@
 // The bias depends on j - i alone.  Streamed rows pass an owner row in order, so the values that the score tiles of an owner
 // tile start from (the accumulators of the score contraction: no vector instruction adds them) are a window of one vector
 // over the distances, which moves on by 64 entries a tile.  It lives in a ring in LDS; a tile's new entries are looked up
-// (bucket, then table) a tile ahead of each other and stored with the tile.  In the forward pass a tile whose pairs, for a wave, all lie at
-// or beyond +-reach starts from zeros, and its one bias is a factor of the constant that the bias of the sequence is.  (B = 4, H = 12,
-// N = 8192, reach 256: TODO us, with all tiles from the ring TODO.  The backward passes gain 1 % by it, for twice the code.)
+// (bucket, then table) some tiles ahead of each other and stored with the tile.  Any reach costs the same.  (A forward pass that started
+// the tiles beyond +-reach, which have one bias, from zeros and took the bias as a factor of the sequence's gained 4 % where nearly all tiles
+// are such, lost 2 % where none are and 11 % in the smallest calls, and had two loops.)
 #pragma once
 #include "sigattn_kernels.hpp"
 
@@ -81,10 +81,6 @@ struct Mods {
     int chunk;                                                 // the 64 entries that are stored next: those of tile `chunk`
     int bucket;
     unsigned short looked_up;
-    int tile_lo, above_from, below_to;                         // lowest distance of the tile in hand; where the far sides begin
-    bool near_tile;
-    float cb_base, cb_above, cb_below, cb_tile;
-
     // dropout
     unsigned keep, key0, key1, c3, c2, row, group;             // row, group: counter words of owner block 0, this block
     unsigned ph[DROP ? QB : 1][4], stays[DROP ? QB : 1];
@@ -120,7 +116,7 @@ struct Mods {
         return d > -n && d < ns ? v : 0.f;
     }
 
-    __device__ __forceinline__ void open(const int z, const int h_, const int n_, const int ns_, const int m0_, const float cb, const float c1) {
+    __device__ __forceinline__ void open(const int z, const int h_, const int n_, const int ns_, const int m0_, const float c1) {
         h = h_; n = n_; ns = ns_; m0 = m0_;
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -133,20 +129,6 @@ struct Mods {
             unit = -1.4426950408889634f / c1;
             chunk = 2;
             bucket = bucket_at(64 * own_chunk() - m0 + lane);
-            if constexpr (MODE == FWD) {
-                // the far sides: where their bias is a factor that fp32 holds with room on both sides (-inf is a mask, and goes through the ring)
-                auto far_cb = [&](const int b) {
-                    const int i = b < 0 ? 0 : (b >= x.num_buckets ? x.num_buckets - 1 : b);
-                    const float f = cb * __builtin_amdgcn_exp2f((float)x.table[(size_t)i * p.H + h] * -1.4426950408889634f);
-                    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
-                };
-                cb_base = cb;
-                cb_above = far_cb(x.buckets[2 * x.reach]);
-                cb_below = far_cb(x.buckets[0]);
-                above_from = cb_above > 0x1p-100f && cb_above < 0x1p100f ? x.reach : 0x7FFFFFFF;
-                below_to = cb_below > 0x1p-100f && cb_below < 0x1p100f ? -x.reach : (int)0x80000000;
-                tile_lo = -(m0 + 32 * QB * wave) - (32 * QB - 1) - start_pos - 64;
-            }
         }
         if constexpr (DROP) {
             keep = __builtin_amdgcn_readfirstlane(x.keep);
@@ -171,18 +153,6 @@ struct Mods {
             below = 0.f;
         }
     }
-    // Forward: goes on to the next tile; whether its scores start from the ring.
-    __device__ __forceinline__ bool next_tile() {
-        tile_lo += 64;
-        const bool above = tile_lo >= above_from, below = tile_lo + 32 * QB + 62 <= below_to;
-        const float a = cb_above, b = cb_below, c = cb_base;    // values: a choice between members would keep them all in memory
-        cb_tile = above ? a : (below ? b : c);
-        near_tile = !above && !below;
-        return near_tile;
-    }
-    __device__ __forceinline__ bool near() const { return near_tile; }
-    __device__ __forceinline__ float cb_of_tile() const { return cb_tile; }
-
     // The waves take turns with the entries of a tile: this wave's first one.
     __device__ __forceinline__ int own_chunk() const { return 2 + ((wave - 2) & (NW - 1)); }
     // The entries of the first two tiles and of the owner tile in front of them.

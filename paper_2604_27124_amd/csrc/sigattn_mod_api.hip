@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const E
 
 // dtable[b][h] for 16 buckets of a head: the entries of all groups (of one group where every sequence has a start of its own), a
 // thousand at a time, with their buckets, in LDS; each wave goes through them for its four buckets.  DIRECT: a few rows,
-// taken as they are, without the launch above (B = 2, H = 2, N = 256: backward TODO -> TODO us); a group is a sequence then.
+// taken as they are, without the launch above (B = 2, H = 2, N = 256: backward 19.7 -> 17.7 us); a group is a sequence then.
 constexpr int TABLE_BUCKETS = 16, TABLE_ENTRIES = 1024, DIRECT_ROWS = 64;
 template <bool DIRECT>
 __global__ void __launch_bounds__(256) sigattn_rel_table(const Lengths l, const Extra x, const int groups, bf16_t *dtable) {

@@ -383,3 +383,22 @@ def test_many_runs_of_large_tiles_give_the_same_bits(op):
     assert bool(torch.isfinite(first).all()) and float(first.float().abs().max()) < 10
     for _ in range(40):
         assert same_bits(c.fwd(), first)
+
+
+@pytest.mark.parametrize("op", ["rel", "dropout", "both"])
+def test_many_short_sequences(op):
+    # batch order in both directions, more sequences than a wave ranks
+    lens = [(13 * i) % 41 for i in range(150)]
+    check(Case(150, 40, 40, 2, 64, lens, lens, op, 12, 9, None, seed=21))
+
+
+def test_what_the_workspace_held_does_not_matter():
+    c = Case(3, 300, 400, 2, 64, (300, 0, 131), (400, 77, 33), "rel", 100, 32, (7, 0, -50), seed=22).upload()
+    want = c.bwd()
+    n = A.sigmoid_attn_rel_bwd_workspace_bytes(3, 300, 400, 2, 64, 100)
+    ws = torch.full((n // 4,), float("nan"), device="cuda")
+    for a, b in zip(c.bwd(workspace=ws), want):
+        assert same_bits(a, b)
+    guard = torch.full((n // 4 + 1024,), 3.0, device="cuda")                # nothing behind its end is written
+    c.bwd(workspace=guard[:n // 4])
+    assert bool((guard[n // 4:] == 3.0).all())

@@ -44,10 +44,8 @@ def kernels(tmp_path_factory):
 
 
 def loops(name):
-    """Passes over the streamed tiles: two in a joint backward kernel; a forward kernel with a bias has a loop for each kind of tile."""
-    if "sigattn_mod_bwd" in name[1]:
-        return 2
-    return 2 if "sigattn_modILi0E" in name[1] and "rel" in name[0] else 1
+    """Passes over the streamed tiles."""
+    return 2 if "sigattn_mod_bwd" in name[1] else 1
 
 
 def test_every_kernel_is_looked_at(kernels):
