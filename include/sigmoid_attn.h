@@ -52,7 +52,9 @@ extern "C" {
 #define SIGATTN_ERR_WORKSPACE (-4)        /* workspace missing or smaller than ..._workspace_bytes()      */
 #define SIGATTN_ERR_LAUNCH (-5)           /* the HIP runtime refused a launch (see hipGetLastError)       */
 #define SIGATTN_ERR_TOO_LARGE (-6)        /* B*H or the tile count exceeds one grid, H*d > 2^20, or more  */
-                                          /* than 256 sequences padded to more than 262144 rows            */
+                                          /* than 256 sequences padded to more than 262144 rows; with a     */
+                                          /* position bias or dropout also more than 2^29 rows, a reach over */
+                                          /* 2^24, more than 65536 buckets                                   */
 
 /* Library version: major * 10000 + minor * 100 + patch. */
 int sigmoid_attn_version(void);

@@ -541,7 +541,8 @@ def sigmoid_attn_rel_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, tabl
 
 def sigmoid_attn_rel_bwd(q, k, v, d_o, seqlens_q, seqlens_k, bias, scale: float, table, buckets, q_start=None, dq=None, dk=None, dv=None,
                          dtable=None, workspace=None, stream=None) -> Tuple:
-    """(dQ, dK, dV, dtable) of sigmoid_attn_rel_fwd.  Outputs and the workspace are allocated if None."""
+    """(dQ, dK, dV, dtable) of sigmoid_attn_rel_fwd.  Outputs and the workspace (sigmoid_attn_rel_bwd_workspace_bytes) are allocated if
+    None; with a stream that is not torch's a workspace has to be passed."""
     if dq is None and dk is None and dv is None and dtable is None and workspace is None and stream is None:
         res = (_fast or _fastcalls()).mod_bwd(1, q, k, v, d_o, seqlens_q, seqlens_k, bias, scale, table, buckets, q_start)
         if res is not None:

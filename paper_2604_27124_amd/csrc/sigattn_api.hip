@@ -230,7 +230,7 @@ int launch_onepass(onepass::Params p, const int per_slice, unsigned char *worksp
 
 extern "C" {
 
-int sigmoid_attn_version(void) { return 400; }
+int sigmoid_attn_version(void) { return 500; }
 
 const char *sigmoid_attn_strerror(int code) {
     switch (code) {
@@ -240,7 +240,7 @@ const char *sigmoid_attn_strerror(int code) {
         case SIGATTN_ERR_MISALIGNED: return "tensor pointer is not 16-byte aligned";
         case SIGATTN_ERR_WORKSPACE: return "workspace missing or too small";
         case SIGATTN_ERR_LAUNCH: return "HIP kernel launch failed";
-        case SIGATTN_ERR_TOO_LARGE: return "problem too large: more workgroups than one launch holds, H*d > 2^20, more than 256 sequences padded beyond 262144 rows, or more query tiles than the static scratch array holds";
+        case SIGATTN_ERR_TOO_LARGE: return "problem too large: more workgroups than one launch holds, H*d > 2^20, more than 256 sequences padded beyond 262144 rows, more query tiles than the static scratch array holds, or beyond a position bias's limits (2^29 rows, reach 2^24, 65536 buckets)";
         default: return "unknown error code";
     }
 }
