@@ -178,17 +178,28 @@ Extra extra(const Bias *rel, const Drop *drop) {
     return x;
 }
 
-// Few queries (sigattn_rel_few.hpp): parts of a (z, h)'s keys.  A part is at least 1024 keys long (its start, and the second launch, take as
-// long as reading some hundreds), and there are no more than give every CU two workgroups.
+// Which calls with a bias and no dropout take the kernel for few queries (sigattn_rel_few.hpp).  It reads the keys once for every
+// eight queries and grows with their number, the tiled kernel takes as long for one query as for 128 and has a workgroup a head.
+// us, d = 64 (d = 128), H = 12, whole context valid, few / tiled:
+//   16 queries, B = 1, 8192 keys   22 / 120  (37 / 177)      8 queries, B = 8, 8192 keys    57 / 121 (108 / 181)
+//   16 queries, B = 8, 8192 keys  105 / 121  (200 / 181)     8 queries, B = 32, 4096 keys  127 / 97  (235 / 237)
+//   16 queries, B = 32, 4096 keys 187 / 97   (350 / 237)     4 queries, B = 32, 4096 keys   89 / 97  (158 / 237)
+// Below some 200 workgroups the tiled kernel leaves CUs idle; beyond, its matrix instructions win from five queries on.
+int few_groups(int L_q) { return (L_q + 7) / 8; }
+bool few_queries(int B, int L_q, int H) {
+    return L_q <= 4 || (L_q <= few::MOST && (long long)B * H * few_groups(L_q) <= 192);
+}
+// Parts of a (z, h)'s keys.  A part is at least 1024 keys long (its start, and the second launch, take as long as reading some hundreds), and
+// there are no more than give every CU two workgroups.  us, d = 64, H = 12, whole / in parts: one query, B = 1, 2048 keys 8.5 / 8.1, 8192
+// keys 33.2 / 9.3; B = 8, 8192 keys 39.8 / 34.7; 16 queries, B = 1, 8192 keys 112 / 22.
 int few_splits(int B, int L_k, int H) {
     const long long room = 512 / ((long long)B * H), longest = ((long long)L_k + 1023) / 1024;
     const long long s = room < longest ? room : longest;
     return s < 1 ? 1 : (int)s;
 }
 int few_rows(int L_q) { return L_q == 1 ? 1 : L_q == 2 ? 2 : L_q <= 4 ? 4 : 8; }
-int few_groups(int L_q) { return (L_q + 7) / 8; }
 size_t few_bytes(int B, int L_q, int L_k, int H, int d) {
-    if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK || L_q > few::MOST) return 0;
+    if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK || !few_queries(B, L_q, H)) return 0;
     const int s = few_splits(B, L_k, H);
     return s == 1 ? 0 : (size_t)s * B * H * few_groups(L_q) * few_rows(L_q) * d * sizeof(float);
 }
@@ -210,7 +221,7 @@ int forward(const void *q, const void *k, const void *v, void *o, const int32_t 
     p.bias = bias; p.scale = scale; p.B = B; p.H = H;
     const Extra x = extra(rel, drop);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (rel && !drop && L_q <= few::MOST) {
+    if (rel && !drop && few_queries(B, L_q, H)) {
         const size_t need = few_bytes(B, L_q, L_k, H, d);
         const bool parts = need > 0 && workspace && workspace_bytes >= need && aligned16(workspace);
         return few::launch(few::Few{p, x, parts ? few_splits(B, L_k, H) : 1, few_groups(L_q), static_cast<float *>(workspace)}, d, s);

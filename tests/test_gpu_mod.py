@@ -128,6 +128,7 @@ SMALL = [
     (1, 13, 2500, 2, (11,), (2400,), 100, 32, (-3,)),
     (2, 400, 700, 1, (400, 333), (700, 650), 30, 32, (100, -60)),
     (40, 150, 90, 7, [150 - 3 * i for i in range(40)], [90 - 2 * i for i in range(40)], 30, 32, None),   # two query blocks a wave
+    (40, 6, 90, 7, [6 - i % 7 for i in range(40)], [90 - 2 * i for i in range(40)], 30, 32, [84 - 3 * i for i in range(40)]),   # many heads of few queries
     (70, 65, 65, 1, [65 - i % 66 for i in range(70)], [65 - i % 66 for i in range(70)], 20, 41, None),
 ]
 
