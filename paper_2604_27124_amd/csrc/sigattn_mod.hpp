@@ -59,8 +59,13 @@ constexpr int FAR = 32;              // floats behind the entries of a row: [0] 
 
 // What one pass adds to a kernel.  BIASED: the position bias; SIFTED: dropout; SUMMED: sums of dS by distance (DQ).  Not SCALED: scores are
 // contracted from the queries and keys as they are and multiplied by scale log2 e in fp32, one instruction more for each.  The
-// results are 2.4e-3 (2-norm) from 64 bits, the rounding of P (dS) and of the result itself, and not 2.9e-3; with dropout the
-// forward pass of B = 8, H = 12, N = 2048 takes 1 % longer, the backward 3 %.
+// results are 2.4e-3 (2-norm) from 64 bits, the rounding of P (dS) and of the result itself, and not 2.9e-3; forward and backward
+// pass of B = 8, H = 12, N = 2048 with dropout take 2 % longer each, of B = 4, H = 12, N = 8192 with a bias 5 % and 3 %.
+//
+// us, forward + backward, beside the plain calls' two-pass kernels (the same lengths): d = 64, B = 8, H = 12, N = 2048, bias 132 + 437
+// (every distance near: 134 + 529), dropout 156 + 468, plain 110 + 366; d = 128, B = 8, H = 16, N = 2048, bias 276 + 1063, both 323 +
+// 1244, plain 245 + 931.  What bounds them is what bounds the plain ones, matrix, vector and LDS work together at the power limit,
+// and the vector instructions that the bias, the generator and the sums add to each score.
 template <int MODE, int QB, int NW, bool BIAS, bool DROP, bool SUM>
 struct Mods {
     static constexpr bool BIASED = BIAS, SIFTED = DROP, SUMMED = SUM, SCALED = false;
@@ -293,7 +298,10 @@ struct Mods {
     // distances 2 u and 2 u + 1 of the block's 63, of an even column 2 u + 1 and 2 u + 2; the rest of a column is zeros.  Columns c % 4 lie in four
     // pieces of scratch, and the 16 lanes that read one add up eight columns, four distances a lane.  The four groups of
     // lanes are joined when the 32 distances that no later block reaches go out; the others move down by as much.
-    // Every sum has its order: no atomics.  (With ds_add_f32 into such a window a block took 16 of them, at about a lane a
+    // Every sum has its order: no atomics.  What is summed is dS as the dQ contraction takes it, rounded to bf16; the sums are fp32.  Roundings of
+    // either sign cancel as the terms do: dtable is 2.5e-3 to 3e-3 (2-norm) from 64 bits, as dQ is, of which its own rounding to bf16 is 1.7e-3; with
+    // terms in fp32 twice the words would go through LDS, which already makes the near blocks 21 % dearer.
+    // (With ds_add_f32 into such a window a block took 16 of them, at about a lane a
     // clock: backward of B = 256, H = 12, N = 512 1657 us.)
     static constexpr int ROW_SHR_1 = 0x111, ROW_SHL_8 = 0x108;
     template <int CTRL>

@@ -270,6 +270,7 @@ int backward(const void *q, const void *k, const void *v, const void *d_o, void 
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (!rel) return d == 64 ? mod::bwd_dropout_64(pk, pq, x, s) : mod::bwd_dropout_128(pk, pq, x, s);
 
+    // Groups of sequences (sigattn_rel_rows): B = 256, H = 12, N = 512 backward 622 us with 16, 632 with 4, 634 with 64.
     const int entries = RowSums::entries(rel->reach, L_q, L_k), groups = rel->q_start || B < 16 ? B : 16;
     const long long row_wgs = (long long)groups * H * (entries / 32 + 1), table_wgs = (long long)H * ((rel->num_buckets + TABLE_BUCKETS - 1) / TABLE_BUCKETS);
     int seqs = 1;
