@@ -183,9 +183,9 @@ int sigmoid_attn_bwd_dq_dbias_static(const void *q, const void *k, const void *v
  *                   with it a call takes the last tokens of a context alone.  Clamped to +-2^29.
  * reach is 0 to 2^24, num_buckets 1 to 65536, L_q and L_k at most 2^29.  An entry of -inf (or the type's lowest value) masks its pairs: P and dS are exact zeros.
  * Entries that no valid pair has influence no output, NaN ones neither.
- * Few padded queries (L_q <= 4, and up to 16 where B * H * ceil(L_q / 8) <= 192) take a forward kernel of their own, whose scores and weights
+ * Few padded queries (L_q <= 4, and up to 64 where L_k > 1024 and B * H * ceil(L_q / 8) <= 128) take a forward kernel of their own, whose scores and weights
  * stay in fp32.  Where few heads share a long context, the keys of a head go to several workgroups, if the forward call has a 16-byte aligned
- * workspace of sigmoid_attn_rel_fwd_workspace_bytes(...) bytes (0: this shape is not split; NULL / 0 is always accepted).  With up to 16 queries
+ * workspace of sigmoid_attn_rel_fwd_workspace_bytes(...) bytes (0: this shape is not split; NULL / 0 is always accepted).  With up to 64 queries
  * the last bits of O depend on all that, with more on nothing but the sequence.
  * The workspace of the backward call (sigmoid_attn_rel_bwd_workspace_bytes(...) bytes, 16-byte aligned, owned by the caller, contents
  * irrelevant on entry and undefined on exit) holds a row of sums by distance for every 32 queries; sums are taken in fp32, in an

@@ -531,7 +531,7 @@ def sigmoid_attn_rel_fwd(q, k, v, seqlens_q, seqlens_k, bias, scale: float, tabl
                          stream=None):
     """Forward pass with table[buckets[clamp(j - i - q_start, -reach, reach) + reach]][h] added to the scores.
     table: bf16 [num_buckets, H]; buckets: int32 [2 * reach + 1] (sigmoid_attn_rel_buckets makes one); q_start: int32 [B] or None.
-    The workspace (for up to 16 queries against a long context) is allocated if None; an empty tensor stands for none."""
+    The workspace (for up to 64 queries against a long context) is allocated if None; an empty tensor stands for none."""
     if out is None and workspace is None and stream is None:
         res = (_fast or _fastcalls()).mod_fwd(1, q, k, v, seqlens_q, seqlens_k, bias, scale, table, buckets, q_start)
         if res is not None:

@@ -179,15 +179,17 @@ Extra extra(const Bias *rel, const Drop *drop) {
 }
 
 // Which calls with a bias and no dropout take the kernel for few queries (sigattn_rel_few.hpp).  It reads the keys once for every
-// eight queries and grows with their number, the tiled kernel takes as long for one query as for 128 and has a workgroup a head.
-// us, d = 64 (d = 128), H = 12, whole context valid, few / tiled:
-//   16 queries, B = 1, 8192 keys   22 / 120  (37 / 177)      8 queries, B = 8, 8192 keys    57 / 121 (108 / 181)
-//   16 queries, B = 8, 8192 keys  105 / 121  (200 / 181)     8 queries, B = 32, 4096 keys  127 / 97  (235 / 237)
-//   16 queries, B = 32, 4096 keys 187 / 97   (350 / 237)     4 queries, B = 32, 4096 keys   89 / 97  (158 / 237)
-// Below some 200 workgroups the tiled kernel leaves CUs idle; beyond, its matrix instructions win from five queries on.
+// eight queries and grows with their number, but can split a head's keys; the tiled kernel takes as long for one query as for 128 and has
+// a workgroup a head.  us, d = 64 (d = 128), H = 12, whole context valid, few / tiled:
+//    1 query,   B = 32, 4096 keys   52 / 97              4 queries, B = 32, 4096 keys   89 / 97  (158 / 237)
+//   16 queries, B = 1, 8192 keys    22 / 120 (37 / 177)  8 queries, B = 8, 8192 keys    57 / 121 (108 / 181)
+//   64 queries, B = 1, 8192 keys    54 / 120 (94 / 177)  64 queries, B = 1, 2048 keys   21 / 33  (36 / 48)
+//   48 queries, B = 2, 2048 keys    39 / 33  (65 / 49)   16 queries, B = 8, 8192 keys  105 / 121 (200 / 181)
+//   16 queries, B = 1, 1000 keys    18 / 19  (29 / 27)   16 queries, B = 1, 64 keys    6.4 / 5.1 (6.4 / 6.4)
+// So it takes five queries and more only where there are keys to split and, without that, less than half of the CUs had work.
 int few_groups(int L_q) { return (L_q + 7) / 8; }
-bool few_queries(int B, int L_q, int H) {
-    return L_q <= 4 || (L_q <= few::MOST && (long long)B * H * few_groups(L_q) <= 192);
+bool few_queries(int B, int L_q, int L_k, int H) {
+    return L_q <= 4 || (L_q <= few::MOST && L_k > 1024 && (long long)B * H * few_groups(L_q) <= 128);
 }
 // Parts of a (z, h)'s keys.  A part is at least 1024 keys long (its start, and the second launch, take as long as reading some hundreds), and
 // there are no more than give every CU two workgroups.  us, d = 64, H = 12, whole / in parts: one query, B = 1, 2048 keys 8.5 / 8.1, 8192
@@ -199,7 +201,7 @@ int few_splits(int B, int L_k, int H) {
 }
 int few_rows(int L_q) { return L_q == 1 ? 1 : L_q == 2 ? 2 : L_q <= 4 ? 4 : 8; }
 size_t few_bytes(int B, int L_q, int L_k, int H, int d) {
-    if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK || !few_queries(B, L_q, H)) return 0;
+    if (check_shape(B, L_q, H, d) != SIGATTN_OK || check_shape(B, L_k, H, d) != SIGATTN_OK || !few_queries(B, L_q, L_k, H)) return 0;
     const int s = few_splits(B, L_k, H);
     return s == 1 ? 0 : (size_t)s * B * H * few_groups(L_q) * few_rows(L_q) * d * sizeof(float);
 }
@@ -221,7 +223,7 @@ int forward(const void *q, const void *k, const void *v, void *o, const int32_t 
     p.bias = bias; p.scale = scale; p.B = B; p.H = H;
     const Extra x = extra(rel, drop);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (rel && !drop && few_queries(B, L_q, H)) {
+    if (rel && !drop && few_queries(B, L_q, L_k, H)) {
         const size_t need = few_bytes(B, L_q, L_k, H, d);
         const bool parts = need > 0 && workspace && workspace_bytes >= need && aligned16(workspace);
         return few::launch(few::Few{p, x, parts ? few_splits(B, L_k, H) : 1, few_groups(L_q), static_cast<float *>(workspace)}, d, s);

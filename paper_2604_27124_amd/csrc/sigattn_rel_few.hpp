@@ -1,4 +1,4 @@
-// Forward pass with a relative position bias for a few queries a sequence, 16 at most: single tokens against a long context.
+// Forward pass with a relative position bias for a few queries a sequence, 64 at most: single tokens against a long context.
 //
 // Every key and value is used by few queries, so the call is bound by reading them once, and matrix instructions, which take
 // 32 queries at a time, would mostly multiply padding.  A wave reads whole rows (d = 64: eight lanes of 16 bytes a row, eight rows a load; d = 128: 16 and
@@ -15,7 +15,7 @@
 namespace sigattn {
 namespace few {
 
-constexpr int NW = 8, THREADS = 64 * NW, MOST = 16;            // most: queries of a sequence, in groups of eight
+constexpr int NW = 8, THREADS = 64 * NW, MOST = 64;            // most: queries of a sequence, in groups of eight
 constexpr int CHUNK = 2048;                                    // keys whose bias is in LDS
 
 template <int CTRL>

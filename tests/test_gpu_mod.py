@@ -126,6 +126,7 @@ SMALL = [
     (3, 8, 131, 3, (8, 7, 0), (131, 128, 5), 30, 12, (123, -4, 0)),
     (2, 2, 64, 2, (2, 1), (0, 64), 3, 5, None),
     (1, 13, 2500, 2, (11,), (2400,), 100, 32, (-3,)),
+    (2, 64, 1100, 1, (64, 37), (1100, 1025), 200, 32, (1036, 0)),
     (2, 400, 700, 1, (400, 333), (700, 650), 30, 32, (100, -60)),
     (40, 150, 90, 7, [150 - 3 * i for i in range(40)], [90 - 2 * i for i in range(40)], 30, 32, None),   # two query blocks a wave
     (40, 6, 90, 7, [6 - i % 7 for i in range(40)], [90 - 2 * i for i in range(40)], 30, 32, [84 - 3 * i for i in range(40)]),   # many heads of few queries

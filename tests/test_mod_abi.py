@@ -53,10 +53,11 @@ def test_sizes(lib):
     # the reach counts only as far as there are distances
     assert size(2, 512, 512, 4, 64, 1 << 20) == size(2, 512, 512, 4, 64, 1 << 24) > size(2, 512, 512, 4, 64, 64)
     few = A.sigmoid_attn_rel_fwd_workspace_bytes
-    assert few(1, 1, 1000, 12, 64) == 0 and few(1, 17, 100000, 1, 64) == 0 and few(1, 0, 9, 1, 64) == 0
+    assert few(1, 1, 1000, 12, 64) == 0 and few(1, 65, 100000, 1, 64) == 0 and few(1, 0, 9, 1, 64) == 0
     assert few(1, 1, 8192, 12, 64) == 8 * 12 * 64 * 4 and few(1, 9, 8192, 1, 128) == 8 * 2 * 8 * 128 * 4
-    # five queries and more of many heads go to the tiled kernels
-    assert few(1, 8, 8192, 192, 64) > 0 and few(1, 8, 8192, 193, 64) == 0 and few(1, 9, 8192, 97, 64) == 0 and few(1, 4, 8192, 193, 64) > 0
+    # five queries and more of many heads, or of few keys, go to the tiled kernels
+    assert few(1, 8, 8192, 128, 64) > 0 and few(1, 8, 8192, 129, 64) == 0 and few(1, 9, 8192, 65, 64) == 0 and few(1, 4, 8192, 193, 64) > 0
+    assert few(1, 64, 1025, 1, 64) > 0 and few(1, 5, 1024, 1, 64) == 0
 
 
 def test_bucket_map_refuses(lib):
