@@ -48,9 +48,9 @@ __device__ __forceinline__ float sum_rows(const Lengths &l, const Extra &x, cons
         t += (a + b) + (e + f);
     }
     for (; ob < to; ob += step) t += rows[ob * stride];
-    // the rows are of dS / cb, without 1 / keep
+    // the rows are of dS / cb, without 1 / keep.  cb / keep may pass fp32 (cb is up to 2^126), where t is zero or nearly so: one after the other.
     const float cb = __builtin_amdgcn_exp2f(__builtin_fminf(__builtin_fmaxf(-l.bias[z] * 1.4426950408889634f, -126.0f), 126.0f));
-    return t * (cb * x.inv_keep);
+    return t * cb * x.inv_keep;
 }
 
 // Sums over rows, in fixed order and without atomics.  Group s of `groups` takes sequences s, s + groups, ...: [group][H][entries + FAR].  A
