@@ -106,6 +106,12 @@ __device__ __forceinline__ float mul_zero_wins(float a, float b) {
     return r;
 }
 
+// The factor of finished gradients, scale 2^(-bias log2 e) and perhaps 1 / keep, is beyond fp32: its parts have to be applied one after the
+// other to the sums, which are as small as the second one is large (or zero: infinity would make them NaN).
+__device__ __forceinline__ bool passes_fp32(float factor) {
+    return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, factor) & 0x7FFFFFFF) == 0x7F800000;
+}
+
 __device__ __forceinline__ unsigned pack_bf16(float a, float b) {
     f32x2 f = {a, b};
     bf16x2 h = __builtin_convertvector(f, bf16x2);   // v_cvt_pk_bf16_f32, round to nearest even
@@ -1106,8 +1112,18 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
         using TL_ACC0 = TrLayout<(MODE == FWD) ? C::LM2 : C::LM1>;      // FWD contracts V^T; DQ K^T; DKDV Q^T (acc0), dO^T (acc1)
         using TL_ACC1 = TrLayout<C::LM2>;
         const float used = Mod::SIFTED ? mod.scale() : 1.0f;            // of the weights
-        const float oscale = used * ((MODE == FWD) ? 1.0f : p.scale * cb);   // dQ and dK carry the factor `scale`; their sums are over dS / cb
-        auto chunk = [&](const f32x16 &a, const int pr, const float f) {   // columns of q4 = 2 pr + g
+        // dQ and dK carry the factor `scale`; their sums are over dS / cb.  The factors are made here for each owner tile: kept
+        // in registers from one to the next they spill.
+        float cb_here = cb;
+        if (MODE != FWD) asm volatile("" : "+s"(cb_here));
+        const float whole = used * ((MODE == FWD) ? 1.0f : p.scale * cb_here);
+        const bool by_parts = MODE != FWD && passes_fp32(whole);
+        const float oscale = by_parts ? used * p.scale : whole, before = by_parts ? cb_here : 1.0f;
+        auto chunk = [&](f32x16 a, const int pr, const float f, const float before) {   // columns of q4 = 2 pr + g
+            if (MODE != FWD) {
+#pragma unroll
+                for (int i = 8 * pr; i < 8 * pr + 8; ++i) a[i] *= before;
+            }
             const unsigned e0 = pack_bf16(a[8 * pr + 0] * f, a[8 * pr + 1] * f), e1 = pack_bf16(a[8 * pr + 2] * f, a[8 * pr + 3] * f);
             const unsigned o0 = pack_bf16(a[8 * pr + 4] * f, a[8 * pr + 5] * f), o1 = pack_bf16(a[8 * pr + 6] * f, a[8 * pr + 7] * f);
             const auto s0 = __builtin_amdgcn_permlane32_swap(e0, o0, false, false);   // {lower half: e0 | o0 of g = 0, upper: of g = 1}
@@ -1136,10 +1152,10 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
             for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
                 for (int pr = 0; pr < 2; ++pr) {
-                    const u32x4 w0 = chunk(acc0[qb][mb], pr, oscale);
+                    const u32x4 w0 = chunk(acc0[qb][mb], pr, oscale, before);
                     __builtin_amdgcn_raw_buffer_store_b128(ok ? w0 : z4, d0, at + 2 * TL_ACC0::out_col(mb, 2 * pr), 0, 0);
                     if (MODE == DKDV) {
-                        const u32x4 w1 = chunk(acc1[MODE == DKDV ? qb : 0][MODE == DKDV ? mb : 0], pr, used);
+                        const u32x4 w1 = chunk(acc1[MODE == DKDV ? qb : 0][MODE == DKDV ? mb : 0], pr, used, 1.0f);
                         __builtin_amdgcn_raw_buffer_store_b128(ok ? w1 : z4, d1, at + 2 * TL_ACC1::out_col(mb, 2 * pr), 0, 0);
                     }
                 }

@@ -230,7 +230,8 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_onepass(const Params p) {
         }
         if (lost) dqa = zero + __builtin_nanf("");
     };
-    const float oscale = p.scale * cb;                                // dQ and dK carry the factor `scale`; their sums are over dS / cb
+    const bool by_parts = passes_fp32(p.scale * cb);
+    const float oscale = by_parts ? p.scale : p.scale * cb;           // dQ and dK carry the factor `scale`; their sums are over dS / cb
     auto dq_end = [&](const int u) {
         if (!last_of_chain) {
             const auto d = __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(reinterpret_cast<const bf16_t *>(part)), 0, TILE_BYTES, 0x00027000);
@@ -247,6 +248,7 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_onepass(const Params p) {
             const int row = 32 * nbq + 16 * (qp >> 4) + 8 * ((qp >> 2) & 1) + 4 * ((qp >> 3) & 1) + (qp & 3);
             const bool ok = u * BN + row < nq;
             const int off = (int)(((unsigned)row * (unsigned)row_stride + 32u * dh + 16u * (l >> 5)) * 2u);
+            if (by_parts) dqa *= cb;                                  // uniform
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 u32x4 w;
@@ -582,6 +584,10 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_onepass(const Params p) {
         const bool ok = m0 + row < nk;
         const int off = (int)(((unsigned)row * (unsigned)row_stride + 8u * (l >> 5)) * 2u);
         const u32x4 z4 = {0u, 0u, 0u, 0u};
+        if (by_parts) {
+            acc0[0] *= cb;
+            acc0[1] *= cb;
+        }
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll

@@ -290,7 +290,8 @@ __device__ __forceinline__ void run_pass(const Params &p, const Work work, unsig
     const int rows = p.N - m0 < BM ? p.N - m0 : BM;
     const int bytes = __builtin_amdgcn_readfirstlane(rows * (int)row_stride * 2);
     const bool ok = m0 + pr * 32 + c < n;
-    const float oscale = MODE == FWD ? 1.0f : p.scale * cb;
+    float oscale = MODE == FWD ? 1.0f : p.scale * cb;
+    if (MODE != FWD && passes_fp32(oscale)) { acc[0] *= cb; oscale = p.scale; }
 #pragma unroll
     for (int o = 0; o < NO; ++o) {
         bf16_t *const out = o == 0 ? p.out0 : p.out1;
