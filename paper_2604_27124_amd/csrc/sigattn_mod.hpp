@@ -350,6 +350,20 @@ struct Mods {
                 t[2] = __builtin_amdgcn_fdot2_f32_bf16(b, one_lo, t[2], false);
                 t[3] = __builtin_amdgcn_fdot2_f32_bf16(b, one_hi, t[3], false);
             }
+            // 0 x Inf and 0 x NaN: a value that is not finite belongs to its own distance alone, not to the other of its word as well.
+            if (__builtin_amdgcn_ballot_w64(__builtin_isunordered(t[0], t[1]) || __builtin_isunordered(t[2], t[3]))) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[i] = 0.f;
+#pragma unroll 1
+                for (int j = 0; j < 8; ++j) {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(get + 128 * j);
+                    const unsigned w0 = w[0], w1 = w[1];
+                    t[0] += __builtin_bit_cast(float, w0 << 16);
+                    t[1] += __builtin_bit_cast(float, w0 & 0xFFFF0000u);
+                    t[2] += __builtin_bit_cast(float, w1 << 16);
+                    t[3] += __builtin_bit_cast(float, w1 & 0xFFFF0000u);
+                }
+            }
             asm volatile("" ::: "memory");
             const bool even = ((lane >> 4) & 1) == 0;          // lanes of even columns are a distance ahead
             const float t3 = moved<ROW_SHR_1>(t[3]);

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from gpu_util import BWD_TOL, to_host
+from mod_oracle import mask
 from test_gpu_mod import Case
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +25,33 @@ def test_a_sequence_that_is_switched_off_adds_zeros(p, d, L):
     dtable, ref = to_host(c.upload().bwd()[3]), c.reference()[4]
     assert np.all(np.isfinite(dtable)), dtable
     assert np.all(off_by(c, dtable, ref) <= 1)
+
+
+@pytest.mark.parametrize("op", ["rel", "both"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_what_is_not_finite_stays_in_its_bucket(bad, d, op):
+    # every distance a bucket of its own; dS of one of them is not finite: a NaN in the table, or +-Inf in dO and V that meet in one pair alone
+    L, R = 90, 40
+    c = Case(1, L, L, 1, d, (L,), (L - 3,), op, R, 2 * R + 1, None, p=0.2, seed=24)
+    if np.isnan(bad):
+        c.table[R + 7] = bad
+        hit = [R + 7]
+    else:
+        # dP = <dO_i, V_j> overflows for query 50 and keys 50 + 7 and 50 + 10 only: both 2^70 in a column that is 0 for all others
+        c.g[0, :, 0, 5], c.v[0, :, 0, 5] = 0.0, 0.0
+        c.g[0, 50, 0, 5], c.v[0, [57, 60], 0, 5] = 2.0 ** 70, (2.0 ** 70, -2.0 ** 70)
+        hit = [R + 7, R + 10]
+    with np.errstate(invalid="ignore"):
+        ref = c.reference()[4]
+        clean = [b for b in range(2 * R + 1) if b not in hit]
+        squares = c.ds_squares()[clean]
+    dtable = to_host(c.upload().bwd()[3]).astype(np.float64)
+    assert np.all(np.isfinite(dtable[clean])), np.argwhere(~np.isfinite(dtable))
+    assert np.all(np.abs(dtable[clean] - ref[clean]) <= BWD_TOL * (np.abs(ref[clean]) + np.sqrt(squares)))
+    stays = mask(*c.rng, 0, L, L, c.p) if op == "both" else np.ones((L, L), bool)
+    for b in hit:                                               # what dropout takes out is not in the sum
+        if np.isnan(bad):
+            assert np.isnan(dtable[b, 0])
+        else:
+            assert np.isinf(dtable[b, 0]) == stays[50, 50 + b - R]
