@@ -4,7 +4,7 @@ import pytest
 
 from gpu_util import BWD_TOL, to_host
 from mod_oracle import mask
-from test_gpu_mod import Case
+from test_gpu_mod import Case, check
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,31 @@ def test_what_is_not_finite_stays_in_its_bucket(bad, d, op):
             assert np.isnan(dtable[b, 0])
         else:
             assert np.isinf(dtable[b, 0]) == stays[50, 50 + b - R]
+
+
+WAYS = {
+    # sequences with starts of their own and more than 64 rows of sums: near, far out on either side, without queries, without keys
+    "starts": dict(B=20, Lq=150, Lk=200, H=2, nq=[150 - 7 * i for i in range(20)], nk=[200, 0, 131, 64] * 5, reach=40, num=16,
+                   start=[0, 50, -60, 199, -149, 1000, -1000, 2 ** 31 - 1, -2 ** 31, 31, 32, 33, -31, -32, -33, 63, 64, 65, 1, 7]),
+    # more than 1024 entries of a row, with and without starts
+    "long rows, starts": dict(B=3, Lq=1000, Lk=700, H=2, nq=(1000, 333, 999), nk=(700, 699, 33), reach=600, num=32, start=(-150, 300, 0)),
+    "long rows": dict(B=3, Lq=1000, Lk=700, H=2, nq=(1000, 333, 999), nk=(700, 699, 33), reach=600, num=32, start=None),
+    # a bucket for every distance
+    "all distances": dict(B=5, Lq=500, Lk=600, H=1, nq=(500, 0, 499, 31, 32), nk=(600, 600, 0, 599, 1), reach=650, num=1301, start=(0, 0, 9, 100, -60)),
+    # groups of sequences, each with several
+    "groups": dict(B=67, Lq=64, Lk=96, H=1, nq=[64 - i % 65 for i in range(67)], nk=[96 - i for i in range(67)], reach=30, num=12, start=None),
+}
+
+
+@pytest.mark.parametrize("op", ["rel", "both"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("way", WAYS)
+def test_every_way_of_adding_up(way, d, op):
+    w = WAYS[way]
+    assert w["B"] * -(-w["Lq"] // 32) > 64                      # not the kernel of a few rows
+    check(Case(w["B"], w["Lq"], w["Lk"], w["H"], d, w["nq"], w["nk"], op, w["reach"], w["num"], w["start"], seed=25))
+
+
+def test_a_long_row_of_few_queries():
+    # more than 1024 entries in the kernel of a few rows
+    check(Case(2, 90, 1500, 2, 64, (90, 77), (1500, 1411), "rel", 1400, 32, (700, -20), seed=26))
