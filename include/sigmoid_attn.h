@@ -226,8 +226,9 @@ int sigmoid_attn_rel_buckets(int32_t *buckets, int num_buckets, int reach);
  * (i, 2 (j div 32) + (j div 4) mod 2, z H + h, offset mod 2^32), gives words r0..r3.  With e = j mod 2 and w = 2 ((j mod 32) div 8) + (j div 2) mod 2 the
  * weight takes bits t = w + 16 e and t + 8 of each word, as the byte a(t) = sum_s 2^s bit(t + 8 (s mod 2), r_(s div 2)), s = 0..7, and
  * m_ij = 1 where 256 a(t) + reversed(a(t xor 16)) + K >= 65536, reversed() turning the order of the eight bits around.  Each weight stays with
- * probability keep exactly.  Weights of keys j and j xor 1 share their two bytes: that both fall has a probability within 8e-5 of (1 - keep)^2,
- * which matters only where p itself is of that size.  All others are independent.
+ * probability keep exactly.  Weights of keys j and j xor 1 share their two bytes: that both fall has a probability of (1 - keep)^2
+ * to (1 - keep)^2 + 8.4e-5, which matters where (1 - keep)^2 itself is not far above that: up to 1.023 times as often as
+ * independent ones from 1 - keep = 0.05 on, 1.13 times from 0.02 on, 1.37 times at 0.01, 15 times at 0.001.  All others are independent.
  */
 int sigmoid_attn_dropout_fwd(const void *q, const void *k, const void *v, void *o,
                              const int32_t *seqlens_q, const int32_t *seqlens_k, const float *bias, float scale,
