@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_onepass(const Params p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 w = {dqa[4 * i], dqa[4 * i + 1], dqa[4 * i + 2], dqa[4 * i + 3]};
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), d, part_off, 1024 * i, SC1);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), d, part_off + 1024 * i, 0, SC1);   // no scalar offset: see the epilogue of run_pass
             }
         } else {
             const int rows = p.L_q - u * BN < BN ? p.L_q - u * BN : BN;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(THREADS, 2) sigattn_onepass(const Params p) {
                 u32x4 w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = ok ? pack_bf16(dqa[8 * i + 2 * e] * oscale, dqa[8 * i + 2 * e + 1] * oscale) : 0u;
-                __builtin_amdgcn_raw_buffer_store_b128(w, d, off, 16 * i, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(w, d, off + 16 * i, 0, 0);
             }
         }
         part += 2 * TILE_BYTES;
