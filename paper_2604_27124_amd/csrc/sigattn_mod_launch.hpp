@@ -71,7 +71,8 @@ int launch_joint(Params kv, Params q, const Extra &x, hipStream_t stream) {
 
 // The shapes, and the rules that choose them, are those of the plain calls, but for the backward pass: d = 64 has an operand ring of
 // four in dK/dV too, which leaves the generator its registers (with eight they spill in the loop).  d = 128 with a bias has
-// a ring of two in dQ (B = 8, H = 16, N = 2048: 1107 -> 1041 us of the backward pass; the sums' registers), and goes in one launch up to 256
+// a ring of two in dQ (B = 8, H = 16, N = 2048: 1107 -> 1041 us of the backward pass; the sums' registers; what is left over goes through scratch, two
+// instructions a tile with the bias alone and 23 with dropout too), and goes in one launch up to 256
 // owner tiles of queries, where two launches would each leave CUs idle (us, one / two: B = 6, H = 4, 513 x 3001 138 / 237; B = 8, H = 16,
 // N = 2048, 2048 tiles, 1243 / 1112).
 inline long long tiles128(const Params &p) { return ((long long)p.N + 127) / 128 * p.B * p.H; }
