@@ -18,7 +18,9 @@
  *
  * over valid i, j only; padded rows of dQ, dK, dV are written as zero.  1 - P is formed without
  * cancellation (as exp(-x) P), so dS keeps its relative accuracy on both saturated tails of sigma,
- * for every score and bias whose exponentials fp32 can hold (|bias| up to about 80).
+ * for every score and bias whose exponentials fp32 can hold.  For P that is |bias| up to about 80.  dS is held divided by
+ * exp(-bias), for a bias far below zero as exp(score + 2 bias) dP, and is zero in the gradients where that is below about exp(-87):
+ * with scores of size 1 from a bias of about -44 on, where dS is exp(-44) dP.  A bias beyond +-87.3 counts as that.
  *
  * Conventions shared by every entry point
  * ---------------------------------------

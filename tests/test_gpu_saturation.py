@@ -44,6 +44,22 @@ def test_switched_off_sequences_have_zero_gradients(B, N, H, d):
     assert bool((dbias[1][1::2] == 0).all())
 
 
+@pytest.mark.parametrize("bias", [-42.0, -60.0, -80.0])
+def test_weights_near_zero(bias):
+    # P keeps its accuracy; dS is held as exp(score + 2 bias) dP, which leaves fp32 between the first two
+    w = W.make(1, 256, 1, 64, (256,), seed=14, bias=[bias])
+    if bias > -44:
+        check_against_oracle(w)
+        return
+    dev = Dev(w)
+    dq, dk, dv = (to_host(a) for a in dev.bwd())
+    import oracle
+    check_slices("O", to_host(dev.fwd()), oracle.fwd(w.q, w.k, w.v, w.seqlens, w.bias, w.scale), w.seqlens, [(0, 0)], FWD_TOL)
+    check_slices("dV", dv, oracle.bwd(w.q, w.k, w.v, w.d_o, w.seqlens, w.bias, w.scale)[2], w.seqlens, [(0, 0)], BWD_TOL)
+    # scores below 6 in size: exp(6 - 120) |dP| is below 2^-149
+    assert not dq.any() and not dk.any()
+
+
 def steep(x, bias, scale, spread, seed):
     """x: an object with q and k.  Scores that make up for the bias: q = k = s in the first column, scale s^2 = -bias, and noise in the others."""
     r = np.random.default_rng(seed)
