@@ -9,7 +9,8 @@
 // The bias depends on j - i alone.  Streamed rows pass an owner row in order, so the values that the score tiles of an owner
 // tile start from (the accumulators of the score contraction: no vector instruction adds them) are a window of one vector
 // over the distances, which moves on by 64 entries a tile.  It lives in a ring in LDS; a tile's new entries are looked up
-// (bucket, then table) some tiles ahead of each other and stored with the tile.  Any reach costs the same.  (A forward pass that started
+// (bucket, then table) some tiles ahead of each other and stored with the tile.  Any reach costs the same here; the sums of dS by distance take longer,
+// and memory, with more of the distances within it (RowSums).  (A forward pass that started
 // the tiles beyond +-reach, which have one bias, from zeros and took the bias as a factor of the sequence's gained 4 % where nearly all tiles
 // are such, lost 2 % where none are and 11 % in the smallest calls, and had two loops.)
 #pragma once
@@ -49,7 +50,9 @@ struct RowSums {
         const int low = 1 - row_blocks;                        // no smaller k exists
         first = first < low ? low : first;
     }
-    // entries of a row (a multiple of 32), for any q_start
+    // entries of a row (a multiple of 32), for any q_start: all of them for every 32 queries, so the rows of a call whose reach is of the order of its
+    // length grow with the square of that (us of the backward pass and MB, B = 4, H = 12, N = 8192, all valid: reach 256 3417, 33; 1024 3645,
+    // 109; 8192 4290, 812)
     __host__ __device__ static int entries(int reach, int L_q, int L_k) {
         const int near = (2 * reach + 62) / 32 + 2, all = (L_q + 31) / 32 + 2 * ((L_k + 63) / 64);
         return 32 * ((near < all ? near : all) + 1);
@@ -62,10 +65,12 @@ constexpr int FAR = 32;              // floats behind the entries of a row: [0] 
 // results are 2.4e-3 (2-norm) from 64 bits, the rounding of P (dS) and of the result itself, and not 2.9e-3; forward and backward
 // pass of B = 8, H = 12, N = 2048 with dropout take 2 % longer each, of B = 4, H = 12, N = 8192 with a bias 5 % and 3 %.
 //
-// us, forward + backward, beside the plain calls' two-pass kernels (the same lengths): d = 64, B = 8, H = 12, N = 2048, bias 132 + 437
-// (every distance near: 134 + 529), dropout 156 + 468, plain 110 + 366; d = 128, B = 8, H = 16, N = 2048, bias 276 + 1063, both 323 +
-// 1244, plain 245 + 931.  What bounds them is what bounds the plain ones, matrix, vector and LDS work together at the power limit,
-// and the vector instructions that the bias, the generator and the sums add to each score.
+// us, forward + backward, beside the plain calls' two-pass kernels (the same lengths): d = 64, B = 8, H = 12, N = 2048, bias 136 + 457
+// (every distance near: 136 + 545), dropout 159 + 490, plain 112 to 128 + 376 to 385; d = 128, B = 8, H = 16, N = 2048, bias 293 + 1101, both 336 +
+// 1309, plain 251 + 973.  What bounds them with dropout is the issue of vector instructions, 17.7 for each matrix instruction of the d = 64 forward pass
+// and 15.8 of the backward for the plain kernels' 7.4 and 8.2: their port is busy 82 and 87 % of the time (plain 69 and 75 %).  With a bias no unit is busy
+// most of the time (vector issue 64 to 67 %, matrix units 35 to 40 %, LDS 35 to 47 %, waves waiting to issue 30 to 34 %).  The clock is 1.9 to 2.1 GHz
+// where the plain kernels' is 1.7 to 1.9: the power limit, which holds those, holds these less.
 template <int MODE, int QB, int NW, bool BIAS, bool DROP, bool SUM>
 struct Mods {
     static constexpr bool BIASED = BIAS, SIFTED = DROP, SUMMED = SUM, SCALED = false;
@@ -300,7 +305,7 @@ struct Mods {
     // lanes are joined when the 32 distances that no later block reaches go out; the others move down by as much.
     // Every sum has its order: no atomics.  What is summed is dS as the dQ contraction takes it, rounded to bf16; the sums are fp32.  Roundings of
     // either sign cancel as the terms do: dtable is 2.5e-3 to 3e-3 (2-norm) from 64 bits, as dQ is, of which its own rounding to bf16 is 1.7e-3; with
-    // terms in fp32 twice the words would go through LDS, which already makes the near blocks 21 % dearer.
+    // terms in fp32 twice the words would go through LDS, which already makes the near blocks 21 % dearer (not built).
     // (With ds_add_f32 into such a window a block took 16 of them, at about a lane a
     // clock: backward of B = 256, H = 12, N = 512 1657 us.)
     static constexpr int ROW_SHR_1 = 0x111, ROW_SHL_8 = 0x108;

@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(256) sigattn_rel_rows(const Lengths l, const E
 }
 
 // dtable[b][h] for 16 buckets of a head: the entries of all groups (of one group where every sequence has a start of its own), a
-// thousand at a time, with their buckets, in LDS; each wave goes through them for its four buckets.  DIRECT: a few rows,
+// thousand at a time, with their buckets, in LDS; each wave goes through them for its four buckets.  (Sequences with starts follow each other here, about 1.7 us
+// each: B = 256, H = 12, N = 512 backward 1182 us without starts, 1605 with; B = 1024, N = 128 558 and 2320.)  DIRECT: a few rows,
 // taken as they are, without the launch above (B = 2, H = 2, N = 256: backward 19.7 -> 17.7 us); a group is a sequence then.
 constexpr int TABLE_BUCKETS = 16, TABLE_ENTRIES = 1024, DIRECT_ROWS = 64;
 template <bool DIRECT>
@@ -192,7 +193,8 @@ bool few_queries(int B, int L_q, int L_k, int H) {
     return L_q <= 4 || (L_q <= few::MOST && L_k > 1024 && (long long)B * H * few_groups(L_q) <= 128);
 }
 // Parts of a (z, h)'s keys.  A part is at least 1024 keys long (its start, and the second launch, take as long as reading some hundreds), and
-// there are no more than give every CU two workgroups.  us, d = 64, H = 12, whole / in parts: one query, B = 1, 2048 keys 8.5 / 8.1, 8192
+// one group of queries has no more than give every CU two workgroups; up to eight groups have as many each (64 queries of 12 heads against
+// 100000 keys: 4032 workgroups).  us, d = 64, H = 12, whole / in parts: one query, B = 1, 2048 keys 8.5 / 8.1, 8192
 // keys 33.2 / 9.3; B = 8, 8192 keys 39.8 / 34.7; 16 queries, B = 1, 8192 keys 112 / 22.
 int few_splits(int B, int L_k, int H) {
     const long long room = 512 / ((long long)B * H), longest = ((long long)L_k + 1023) / 1024;
